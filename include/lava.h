@@ -70,6 +70,10 @@ typedef enum lava_budget_mode {
 #define LAVA_DEV_BUDGET_INFEASIBLE 2u /* total budget outside [L*floor, L*cap]; was clamped  */
 #define LAVA_DEV_WAIT_EXPIRED 4u      /* a bounded wait inside a kernel gave up              */
 #define LAVA_DEV_BAD_SEQLEN 8u        /* some sequence is longer than desc->max_seqlen       */
+#define LAVA_DEV_PAGES_EXHAUSTED 16u  /* lava_page_admit / _extend: fewer free pages than needed,
+                                         nothing was changed                                     */
+#define LAVA_DEV_BAD_ROWS 32u         /* lava_page_admit / _extend: a row count outside the head's
+                                         row of the page table, nothing was changed              */
 
 /* Variants of the method (the ablation of Sec. 5.4 and the score functions of the methods the
  * paper compares with).  0 is LAVa as published. */
@@ -362,6 +366,158 @@ LAVA_API lava_status lava_decode_attention(const lava_layer_desc* desc, const vo
                                            const int32_t* head_offsets,
                                            const int64_t* layer_row_offset, float* out,
                                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* Paged cache -- the compressed cache of a model that goes on decoding.  The packed cache of
+ * lava_compact_kv has no room for new tokens; here every (layer, sequence, KV head) -- a "head"
+ * below -- holds its rows in pages of `page_rows` rows out of one pool, so heads of any length
+ * grow row by row, and sequences come and go.
+ *   k_pages, v_pages  [n_pages, page_rows, head_dim], dtype
+ *   head_rows   int32 [n_layers, batch, H_kv]: rows that a head holds
+ *   page_table  int32 [n_layers, batch, H_kv, max_pages]: row j of a head is row j % page_rows of
+ *               page page_table[head][j / page_rows]; entries behind the last page are not read
+ *   free_pages  int32 [n_pages], a ring of the numbers of the free pages, and
+ *   counters    int64 [2] {taken, given}: the free pages are the entries taken ... given-1, modulo
+ *               n_pages.  At the start: free_pages = 0 ... n_pages-1, counters = {0, n_pages}.
+ *   slots       row numbers in the pool, page * page_rows + row in it; -1: no row
+ * Rows of a page behind a head's last one are never read into a result, whatever they hold.  Page
+ * numbers and row numbers outside the pool are skipped where rows are written and read as zeros.
+ *
+ * A step of a model: lava_page_extend once for all layers, then in each layer lava_rotary_append
+ * and lava_decode_attention_pages.  A new prompt: steps 1 to 3 above, lava_page_admit,
+ * lava_compact_kv_pages. */
+typedef struct lava_cache_desc {
+  int32_t n_layers;
+  int32_t batch;       /* sequences that the cache has room for                             */
+  int32_t n_q_heads;   /* a multiple of n_kv_heads                                          */
+  int32_t n_kv_heads;  /* at most 128                                                       */
+  int32_t head_dim;    /* 64 or 128                                                         */
+  int32_t dtype;       /* lava_dtype of the pages, the queries and the attention's output   */
+  int32_t page_rows;   /* 16, 32, 64, 128 or 256                                            */
+  int32_t max_pages;   /* pages of a head at most = row length of page_table                */
+  int64_t n_pages;     /* pages of the pool; n_pages * page_rows < 2^31                     */
+  float sm_scale;      /* logit scale; 0 => 1/sqrt(head_dim)                                */
+  float softcap;       /* 0 => none; else a logit x becomes softcap * tanh(x / softcap)     */
+} lava_cache_desc;
+
+/* Bytes of `workspace` for the paged calls of this cache: a status word (first 256 bytes, as in
+ * lava_workspace_bytes), and what the attention's blocks exchange.  The caller zeroes it once after
+ * allocating it; every call leaves it ready for the next.  Calls that may run at the same time need
+ * a workspace each.  0 and lava_last_error() for an invalid descriptor. */
+LAVA_API size_t lava_cache_workspace_bytes(const lava_cache_desc* cache);
+
+/* Page tables from row counts.  Both take the pages that they need from the ring in the order of the
+ * heads (layer, sequence, KV head), then of their rows; both change nothing, set a bit of
+ * *status_word (device, may be NULL) and give -1 for every new row where the free pages do not
+ * suffice or a count does not fit.
+ *   lava_page_admit   the selection of new prompts: sequences first_seq ... first_seq + n_seqs - 1
+ *       of the cache get head_offsets[l][s][g+1] - head_offsets[l][s][g] more rows (head_offsets
+ *       [n_layers, n_seqs, H_kv+1] as written by lava_select_topk_layers).
+ *       first_row   out int32 [n_layers, n_seqs, H_kv]: where a head's new rows start
+ *   lava_page_extend  a decode step: every head of sequence b gets add[b] more rows (device int32
+ *       [batch], 0 ... max_add), or, where add[b] < 0, gives all its pages back and holds no rows.
+ *       Pages that are given back can be taken by the next call.
+ *       slots       out int32 [n_layers, batch, max_add, H_kv]: the places of the new rows
+ * head_rows_out and counters_out may be head_rows and counters.  page_table is written where heads
+ * get new pages, free_pages where pages are given back. */
+LAVA_API lava_status lava_page_admit(const lava_cache_desc* cache, int32_t first_seq, int32_t n_seqs,
+                                     const int32_t* head_offsets, const int32_t* head_rows,
+                                     int32_t* head_rows_out, int32_t* page_table,
+                                     const int32_t* free_pages, const int64_t* counters,
+                                     int64_t* counters_out, int32_t* first_row,
+                                     uint32_t* status_word, void* stream);
+LAVA_API lava_status lava_page_extend(const lava_cache_desc* cache, const int32_t* add, int32_t max_add,
+                                      const int32_t* head_rows, int32_t* head_rows_out,
+                                      int32_t* page_table, int32_t* free_pages,
+                                      const int64_t* counters, int64_t* counters_out,
+                                      int32_t* slots, uint32_t* status_word, void* stream);
+
+/* lava_compact_kv_layers into pages: the kept rows of desc->batch sequences (in the cache from
+ * first_seq on) and of all layers of the cache go, bit for bit, to rows first_row[head] ... of their
+ * heads.  desc and cache agree in KV heads, head_dim and dtype.  Heads with first_row < 0 are left
+ * out; rows that are not named are not written. */
+LAVA_API lava_status lava_compact_kv_pages(const lava_layer_desc* desc, const lava_cache_desc* cache,
+                                           int32_t first_seq, const void* k, const void* v,
+                                           int64_t k_layer_stride, int64_t v_layer_stride,
+                                           const int32_t* keep_idx, const int32_t* head_offsets,
+                                           const int32_t* first_row, const int32_t* page_table,
+                                           void* k_pages, void* v_pages, void* stream);
+
+/* Rotary positions.  Pair i of a vector's leading rotary_dim elements turns by the angle
+ * positions[token] * freqs[i]:  (a, b) -> scale * (a cos - b sin, b cos + a sin); the other elements
+ * are copied.  Pairs are (i, i + rotary_dim/2), or (2i, 2i+1) where `interleaved`.  Angles are reduced
+ * in 64 bits, so far positions lose nothing; vectors are turned in fp32 and rounded once.
+ * `backward` turns by the negative angles with the same scale: the gradient with respect to the input
+ * of a gradient with respect to the output (the rotation's transpose), and where scale is 1 what undoes
+ * the rotation. */
+typedef struct lava_rotary_desc {
+  int32_t head_dim;    /* 64 or 128                                  */
+  int32_t rotary_dim;  /* a multiple of 16, 0 ... head_dim           */
+  int32_t interleaved; /* 0 or 1                                     */
+  int32_t backward;    /* 0 or 1                                     */
+  int32_t dtype;       /* lava_dtype of all vectors                  */
+  float scale;         /* factor of the rotated vectors; 0 => 1      */
+} lava_rotary_desc;
+
+typedef enum lava_rotary_kind {
+  LAVA_ROTARY_PLAIN = 0,  /* f_i = base^(-2i/r), r = rotary_dim (RoFormer)                            */
+  LAVA_ROTARY_LINEAR = 1, /* f_i / factor: positions interpolated                                      */
+  LAVA_ROTARY_BASE = 2,   /* the base times factor^(r/(r-2)) (NTK-aware)                               */
+  LAVA_ROTARY_BANDS = 3,  /* wavelengths above original_length/low are divided by factor, those below
+                             original_length/high are kept, a line in 1/wavelength between (Llama 3.1) */
+  LAVA_ROTARY_RAMP = 4    /* pairs that turn more than `high` times in original_length are kept, those
+                             below `low` turns are divided by factor, a line over the pairs' numbers
+                             between (YaRN); scale = 0.1 ln(factor) + 1                                */
+} lava_rotary_kind;
+
+/* freqs (HOST double [rotary_dim/2]) and *scale (HOST, may be NULL) of a kind.  factor >= 1; low and
+ * high (0 < low < high) are read by BANDS and RAMP, original_length > 0 too.  No device work. */
+LAVA_API lava_status lava_rotary_freqs(int32_t kind, int32_t rotary_dim, double base, double factor,
+                                       double original_length, double low, double high,
+                                       double* freqs, float* scale);
+
+/* Queries and keys of n_tokens tokens, each [tokens][heads][head_dim] by its own strides in elements
+ * (out strides may differ from in strides: the output can be laid out as lava_score_layer reads it).
+ * positions: device int32 [n_tokens]; freqs: DEVICE double [rotary_dim/2].  q and q_out, or k and k_out,
+ * may both be NULL.  An output may be its own input (same pointer and strides), else it overlaps no input. */
+LAVA_API lava_status lava_rotary(const lava_rotary_desc* rotary, const double* freqs, int64_t n_tokens,
+                                 const int32_t* positions,
+                                 const void* q, int32_t n_q_heads, int64_t q_stride_tok, int64_t q_stride_head,
+                                 void* q_out, int64_t q_out_stride_tok, int64_t q_out_stride_head,
+                                 const void* k, int32_t n_kv_heads, int64_t k_stride_tok, int64_t k_stride_head,
+                                 void* k_out, int64_t k_out_stride_tok, int64_t k_out_stride_head,
+                                 void* stream);
+
+/* The same for new tokens of a running model: queries turned into q_out (contiguous
+ * [n_tokens, H_q, head_dim]), keys turned and values as they are into the rows that `slots` names
+ * (int32 [n_tokens, H_kv]: layer `layer` of lava_page_extend's slots, n_tokens = batch * max_add).
+ * A token's rows with slot -1 are not written; its queries are turned all the same. */
+LAVA_API lava_status lava_rotary_append(const lava_rotary_desc* rotary, const double* freqs,
+                                        const lava_cache_desc* cache, int64_t n_tokens,
+                                        const int32_t* positions,
+                                        const void* q, int64_t q_stride_tok, int64_t q_stride_head,
+                                        void* q_out,
+                                        const void* k, int64_t k_stride_tok, int64_t k_stride_head,
+                                        const void* v, int64_t v_stride_tok, int64_t v_stride_head,
+                                        const int32_t* slots, void* k_pages, void* v_pages, void* stream);
+
+/* lava_decode_attention over the pages: one new token per sequence, query head h reads KV head
+ * g = h / (H_q / H_kv) of its sequence:
+ *     x_i = sm_scale * q[h] . K_g[i]   (capped where softcap > 0),   i < head_rows
+ *     out[h] = softmax_i(x_i) V_g,     lse[h] = ln sum_i exp(x_i)
+ * for layers first_layer ... first_layer + n_layers - 1 in one call.
+ *   q, out      [n_layers, batch, H_q, d], dtype cache->dtype
+ *   lse         float [n_layers, batch, H_q], may be NULL
+ *   page_table, head_rows   of the whole cache
+ *   workspace   lava_cache_workspace_bytes(cache) bytes, zeroed once
+ * A head without rows gives zeros and lse = -infinity.  Sums, maxima and the output before its last
+ * rounding are fp32; with bf16 the probabilities enter the product with V as two bf16 terms (relative
+ * error below 2^-16).  The split of the rows over blocks depends on all row counts of the call, so the
+ * last bits may too; the same call gives the same bits. */
+LAVA_API lava_status lava_decode_attention_pages(const lava_cache_desc* cache, int32_t first_layer,
+                                                 int32_t n_layers, const void* q, const void* k_pages,
+                                                 const void* v_pages, const int32_t* page_table,
+                                                 const int32_t* head_rows, void* out, float* lse,
+                                                 void* workspace, size_t workspace_bytes, void* stream);
 
 /* Layer-wide selection (Algorithm 1, Evict) with the KV heads of a layer split over several GPUs.
  * Every rank describes its own heads (desc->n_kv_heads = local heads, scores of the local heads in

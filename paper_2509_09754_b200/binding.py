@@ -37,6 +37,25 @@ class _CDesc(ctypes.Structure):
     ]
 
 
+class _CCache(ctypes.Structure):
+    _fields_ = [
+        ("n_layers", ctypes.c_int32), ("batch", ctypes.c_int32),
+        ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("page_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+        ("n_pages", ctypes.c_int64),
+        ("sm_scale", ctypes.c_float), ("softcap", ctypes.c_float),
+    ]
+
+
+class _CRotary(ctypes.Structure):
+    _fields_ = [
+        ("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32), ("backward", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+    ]
+
+
 class _CCascadeView(ctypes.Structure):
     _fields_ = [
         ("layers_done", ctypes.c_int32), ("k_out", ctypes.c_void_p), ("v_out", ctypes.c_void_p),
@@ -124,6 +143,19 @@ def load_library():
     lib.lava_cascade_step.argtypes = [vp, vp, vp, vp, vp, vp, sz, vp]
     lib.lava_cascade_get.argtypes = [vp, ctypes.POINTER(_CCascadeView)]
     for name in ("lava_cascade_create", "lava_cascade_begin", "lava_cascade_step", "lava_cascade_get"):
+        getattr(lib, name).restype = i32
+    cp, rp, f64 = ctypes.POINTER(_CCache), ctypes.POINTER(_CRotary), ctypes.c_double
+    lib.lava_cache_workspace_bytes.restype = sz
+    lib.lava_cache_workspace_bytes.argtypes = [cp]
+    lib.lava_page_admit.argtypes = [cp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.lava_page_extend.argtypes = [cp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.lava_compact_kv_pages.argtypes = [dp, cp, i32, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp]
+    lib.lava_rotary_freqs.argtypes = [i32, i32, f64, f64, f64, f64, f64, vp, vp]
+    lib.lava_rotary.argtypes = [rp, vp, i64, vp] + 2 * [vp, i32, i64, i64, vp, i64, i64] + [vp]
+    lib.lava_rotary_append.argtypes = [rp, vp, cp, i64, vp, vp, i64, i64, vp, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp]
+    lib.lava_decode_attention_pages.argtypes = [cp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    for name in ("lava_page_admit", "lava_page_extend", "lava_compact_kv_pages", "lava_rotary_freqs",
+                 "lava_rotary", "lava_rotary_append", "lava_decode_attention_pages"):
         getattr(lib, name).restype = i32
     for name in ("lava_poll_status", "lava_wo_norm", "lava_score_layer", "lava_score_layers",
                  "lava_layer_budgets", "lava_select_topk", "lava_select_topk_layers",
@@ -402,6 +434,17 @@ class EvictionPlan:
             workspace=ws)
 
 
+def evict_scores(plan: EvictionPlan, q_win, k, v, mode: int = LAVA_BUDGET_DYNAMIC, stream=None) -> None:
+    """Steps 1 to 3 of a full-model eviction: scores, budgets and the selection, as in evict_model."""
+    d, nl = plan.desc, plan.n_layers
+    lava_score_layers(d, nl, q_win, k, v, q_win.stride(0), k.stride(0), v.stride(0), None,
+                      plan.scores, plan.vbar, plan.entropy, plan.workspace, stream)
+    lava_layer_budgets(nl, d.batch, plan.entropy, plan.total_budget, plan.floor, plan.cap, mode,
+                       plan.layer_budget, plan.layer_row_offset, plan.workspace, stream)
+    lava_select_topk_layers(d, nl, plan.scores, plan.layer_budget, plan.keep_idx,
+                            plan.head_offsets, plan.workspace, stream)
+
+
 def evict_model(plan: EvictionPlan, q_win, k, v, mode: int = LAVA_BUDGET_DYNAMIC,
                 stream=None) -> None:
     """One full-model eviction: score all layers, budgets, layer-wide top-k, compaction.
@@ -410,12 +453,7 @@ def evict_model(plan: EvictionPlan, q_win, k, v, mode: int = LAVA_BUDGET_DYNAMIC
     Four library calls, all enqueued on the current stream; nothing is computed in Python.
     """
     d, nl = plan.desc, plan.n_layers
-    lava_score_layers(d, nl, q_win, k, v, q_win.stride(0), k.stride(0), v.stride(0), None,
-                      plan.scores, plan.vbar, plan.entropy, plan.workspace, stream)
-    lava_layer_budgets(nl, d.batch, plan.entropy, plan.total_budget, plan.floor, plan.cap, mode,
-                       plan.layer_budget, plan.layer_row_offset, plan.workspace, stream)
-    lava_select_topk_layers(d, nl, plan.scores, plan.layer_budget, plan.keep_idx,
-                            plan.head_offsets, plan.workspace, stream)
+    evict_scores(plan, q_win, k, v, mode, stream)
     lava_compact_kv_layers(d, nl, k, v, k.stride(0), v.stride(0), plan.keep_idx,
                            plan.head_offsets, plan.layer_row_offset, plan.k_out, plan.v_out,
                            stream)

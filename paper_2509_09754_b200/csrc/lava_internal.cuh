@@ -116,10 +116,19 @@ cudaError_t launch_in_order(void (*kernel)(P...), dim3 grid, dim3 block, size_t 
   return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
+// Geometry of a paged cache handed to kernels by value.
+struct Cache {
+  int n_layers, batch, n_q_heads, n_kv_heads, group, head_dim, dtype;
+  int page_rows, page_shift, max_pages, n_pages;
+  int heads;  // n_layers * batch * n_kv_heads
+  float scale, softcap;
+};
+
 // Host-side error plumbing.
 lava_status fail(lava_status st, const char* fmt, ...);
 lava_status check_cuda(cudaError_t e, const char* what);
 lava_status make_geom(const lava_layer_desc* d, Geom* out);
+lava_status make_cache(const lava_cache_desc* d, Cache* out);
 void count_launches(int n);  // bookkeeping for lava_launch_count()
 
 // lava_score_layers with the layout chosen by the caller; `need` is the least workspace that is accepted.
@@ -215,5 +224,9 @@ lava_status launch_compact(const Geom& g, int n_layers, const void* k, const voi
                            long long k_ls, long long v_ls, const int* keep_idx,
                            const int* head_offsets, const long long* row_off, void* k_out,
                            void* v_out, cudaStream_t stream);
+lava_status launch_compact_pages(const Geom& g, const Cache& c, int first_seq, const void* k, const void* v,
+                                 long long k_ls, long long v_ls, const int* keep_idx, const int* head_offsets,
+                                 const int* first_row, const int* page_table, void* k_pages, void* v_pages,
+                                 cudaStream_t stream);
 
 }  // namespace lava

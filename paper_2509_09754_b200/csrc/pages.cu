@@ -1,0 +1,352 @@
+// Paged cache: descriptors, and the page tables of heads that get rows or give their pages back.
+//
+// A head (layer, sequence, KV head) with r rows holds ceil(r / page_rows) pages.  The heads that grow take
+// the next free pages of the ring in the order of the heads; where a head's pages start is therefore an
+// exclusive prefix sum of what the heads before it need, and so is the place of the pages that go back.
+// Whether all can be served has to be known before anything is written.
+//
+// One cluster: a CTA takes a range of consecutive heads, sums what they need and give, the CTAs read one
+// another's sums behind one cluster barrier, and each writes what its heads get.  Bound by latency: counters
+// and counts, barrier, ring, table.
+#include <algorithm>
+
+#include <cooperative_groups.h>
+
+#include "lava_internal.cuh"
+
+namespace lava {
+
+lava_status make_cache(const lava_cache_desc* d, Cache* out) {
+  if (!d) return fail(LAVA_ERR_INVALID_ARG, "cache is NULL");
+  if (d->n_layers < 1 || d->batch < 1) return fail(LAVA_ERR_INVALID_ARG, "n_layers and batch must be >= 1");
+  if (d->n_kv_heads < 1 || d->n_q_heads < 1 || d->n_q_heads % d->n_kv_heads != 0)
+    return fail(LAVA_ERR_INVALID_ARG, "n_q_heads (%d) must be a positive multiple of n_kv_heads (%d)",
+                d->n_q_heads, d->n_kv_heads);
+  if (d->n_kv_heads > 128) return fail(LAVA_ERR_UNSUPPORTED, "n_kv_heads > 128");
+  if (d->n_q_heads > 65535) return fail(LAVA_ERR_UNSUPPORTED, "n_q_heads > 65535");
+  if (d->head_dim != 64 && d->head_dim != 128)
+    return fail(LAVA_ERR_UNSUPPORTED, "head_dim must be 64 or 128 (got %d)", d->head_dim);
+  if (d->dtype != LAVA_F32 && d->dtype != LAVA_BF16)
+    return fail(LAVA_ERR_INVALID_ARG, "unknown dtype %d", d->dtype);
+  if (d->page_rows != 16 && d->page_rows != 32 && d->page_rows != 64 && d->page_rows != 128 &&
+      d->page_rows != 256)
+    return fail(LAVA_ERR_UNSUPPORTED, "page_rows must be 16, 32, 64, 128 or 256 (got %d)", d->page_rows);
+  if (d->max_pages < 1 || d->n_pages < 1)
+    return fail(LAVA_ERR_INVALID_ARG, "max_pages and n_pages must be >= 1");
+  if (d->n_pages > 0x7fffffffLL / d->page_rows || d->max_pages > 0x7fffffff / d->page_rows)
+    return fail(LAVA_ERR_UNSUPPORTED, "rows of the pool and of a head must fit in 31 bits");
+  const long long heads = (long long)d->n_layers * d->batch * d->n_kv_heads;
+  if ((long long)d->n_layers * d->batch > (1 << 24) || heads > (1 << 24))
+    return fail(LAVA_ERR_UNSUPPORTED, "more than 2^24 heads");
+  if (!(d->sm_scale >= 0.f) || !(d->softcap >= 0.f) || isinf(d->sm_scale) || isinf(d->softcap))
+    return fail(LAVA_ERR_INVALID_ARG, "sm_scale and softcap must be finite and >= 0");
+  Cache c;
+  c.n_layers = d->n_layers;
+  c.batch = d->batch;
+  c.n_q_heads = d->n_q_heads;
+  c.n_kv_heads = d->n_kv_heads;
+  c.group = d->n_q_heads / d->n_kv_heads;
+  c.head_dim = d->head_dim;
+  c.dtype = d->dtype;
+  c.page_rows = d->page_rows;
+  c.page_shift = 0;
+  while ((1 << c.page_shift) < d->page_rows) ++c.page_shift;
+  c.max_pages = d->max_pages;
+  c.n_pages = (int)d->n_pages;
+  c.heads = (int)heads;
+  c.scale = d->sm_scale > 0.f ? d->sm_scale : (float)(1.0 / sqrt((double)d->head_dim));
+  c.softcap = d->softcap;
+  *out = c;
+  return LAVA_OK;
+}
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kThreads = 1024;
+constexpr int kMostCtas = 8;
+
+struct TableParams {
+  Cache c;
+  const int* head_offsets;  // admit: [n_layers, n_seqs, H_kv + 1]
+  int first_seq, n_seqs;
+  const int* add;           // extend: [batch]
+  int max_add;
+  const int* rows;
+  int* rows_out;
+  int* table;
+  const int* ring;
+  int* ring_out;
+  const long long* counters;
+  long long* counters_out;
+  int* first_row;
+  int* slots;
+  unsigned* status;
+};
+
+// What a call does to a head: the pages that it holds, takes and gives back, its rows before and after.
+struct Change {
+  int held, take, give, before, after, bad;
+};
+
+__device__ __forceinline__ Change change_of(const TableParams& p, int h) {
+  const Cache& c = p.c;
+  Change x;
+  x.before = p.rows[h];
+  const int prob = h / c.n_kv_heads, g = h - prob * c.n_kv_heads, layer = prob / c.batch, b = prob - layer * c.batch;
+  long long add = 0;
+  bool ok = true;
+  if (p.add) {
+    add = p.add[b];
+    ok = add <= p.max_add;
+  } else if (b >= p.first_seq && b < p.first_seq + p.n_seqs) {
+    const int* o = p.head_offsets + ((size_t)layer * p.n_seqs + (b - p.first_seq)) * (c.n_kv_heads + 1) + g;
+    add = (long long)o[1] - o[0];
+    ok = add >= 0;
+  }
+  const long long most = (long long)c.max_pages << c.page_shift;
+  const bool release = p.add && add < 0;
+  const long long after = release ? 0 : x.before + add;
+  x.bad = !ok || x.before < 0 || x.before > most || after > most;
+  x.after = (int)after;
+  x.held = x.bad ? 0 : (x.before + c.page_rows - 1) >> c.page_shift;
+  x.take = x.bad || release ? 0 : ((x.after + c.page_rows - 1) >> c.page_shift) - x.held;
+  x.give = x.bad || !release ? 0 : x.held;
+  return x;
+}
+
+struct Sums {
+  long long take, give;
+  int bad;
+};
+
+// Inclusive prefix sums over the block of two values; the totals in *sum.
+__device__ __forceinline__ longlong2 scan_block(int take, int give, longlong2* warps, longlong2* sum) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  long long a = take, b = give;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long x = __shfl_up_sync(0xffffffffu, a, o), y = __shfl_up_sync(0xffffffffu, b, o);
+    if (lane >= o) {
+      a += x;
+      b += y;
+    }
+  }
+  if (lane == 31) warps[warp] = make_longlong2(a, b);
+  __syncthreads();
+  longlong2 before = make_longlong2(0, 0), all = make_longlong2(0, 0);
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w == warp) before = all;
+    all.x += warps[w].x;
+    all.y += warps[w].y;
+  }
+  __syncthreads();
+  *sum = all;
+  return make_longlong2(a + before.x, b + before.y);
+}
+
+__global__ void __launch_bounds__(kThreads)
+page_table_kernel(const TableParams p) {
+  in_stream_order();
+  __shared__ longlong2 warps[kThreads / 32];
+  __shared__ Sums mine;
+  __shared__ int ends[kThreads], held_at[kThreads];  // of the heads in hand: page numbers up to here, pages held
+  const Cache& c = p.c;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x, ctas = gridDim.x, rank = blockIdx.x;
+  const int share = (c.heads + ctas - 1) / ctas;
+  const int h0 = min(c.heads, rank * share), h1 = min(c.heads, h0 + share);
+  const long long taken = p.counters[0], given = p.counters[1];
+
+  // ---- what this CTA's heads need ---------------------------------------------------------------
+  long long take = 0, give = 0;
+  int bad = 0;
+  for (int h = h0 + tid; h < h1; h += kThreads) {
+    const Change x = change_of(p, h);
+    take += x.take;
+    give += x.give;
+    bad |= x.bad;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    take += __shfl_xor_sync(0xffffffffu, take, o);
+    give += __shfl_xor_sync(0xffffffffu, give, o);
+  }
+  if ((tid & 31) == 0) warps[tid >> 5] = make_longlong2(take, give);
+  bad = __syncthreads_or(bad);
+  if (tid == 0) {
+    Sums s = {0, 0, bad};
+    for (int w = 0; w < kThreads / 32; ++w) {
+      s.take += warps[w].x;
+      s.give += warps[w].y;
+    }
+    mine = s;
+  }
+  cluster.sync();
+  long long take_at = 0, give_at = 0, take_all = 0, give_all = 0;
+  bad = 0;
+  for (int r = 0; r < ctas; ++r) {
+    const Sums s = *cluster.map_shared_rank(&mine, r);
+    if (r == rank) {
+      take_at = take_all;
+      give_at = give_all;
+    }
+    take_all += s.take;
+    give_all += s.give;
+    bad |= s.bad;
+  }
+  const bool short_of = taken < 0 || given < taken || given - taken > c.n_pages || take_all > given - taken;
+  // (more pages given back than the pool has in use: the table and the counters do not belong together)
+  if (!short_of && give_all > c.n_pages - (given - taken)) bad = 1;
+  const bool refused = bad || short_of;
+
+  // ---- what they get: 1024 heads at a time --------------------------------------------------------
+  for (int at = h0; at < h1; at += kThreads) {
+    const int h = at + tid;
+    const bool live = h < h1;
+    Change x = {0, 0, 0, 0, 0, 0};
+    if (live) x = change_of(p, h);
+    longlong2 sum;
+    const longlong2 incl = scan_block(x.take, x.give, warps, &sum);
+    const long long first = taken + take_at + incl.x - x.take;  // in the ring
+    if (live) {
+      p.rows_out[h] = refused ? x.before : x.after;
+      const int prob = h / c.n_kv_heads, g = h - prob * c.n_kv_heads, layer = prob / c.batch, b = prob - layer * c.batch;
+      if (p.first_row && b >= p.first_seq && b < p.first_seq + p.n_seqs)
+        p.first_row[((size_t)layer * p.n_seqs + (b - p.first_seq)) * c.n_kv_heads + g] = refused ? -1 : x.before;
+      if (p.slots) {
+        const int n = refused ? 0 : max(0, x.after - x.before);
+        for (int j = 0; j < p.max_add; ++j) {
+          int slot = -1;
+          if (j < n) {
+            const int row = x.before + j, pg = row >> c.page_shift;
+            const int page = pg < x.held ? p.table[(size_t)h * c.max_pages + pg]
+                                         : p.ring[(first + pg - x.held) % c.n_pages];
+            slot = page < 0 || page >= c.n_pages ? -1 : (page << c.page_shift) + (row & (c.page_rows - 1));
+          }
+          p.slots[((size_t)prob * p.max_add + j) * c.n_kv_heads + g] = slot;
+        }
+      }
+    }
+    if (!refused && sum.x > 0) {  // new pages: a thread per page, whose head is found in the sums
+      ends[tid] = (int)incl.x;
+      held_at[tid] = x.held;
+      __syncthreads();
+      for (int e = tid; e < (int)sum.x; e += kThreads) {
+        int lo = 0, hi = kThreads - 1;  // the first head whose pages end behind e
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (ends[mid] > e) hi = mid; else lo = mid + 1;
+        }
+        const int in_head = e - (lo ? ends[lo - 1] : 0);
+        p.table[(size_t)(at + lo) * c.max_pages + held_at[lo] + in_head] = p.ring[(taken + take_at + e) % c.n_pages];
+      }
+      __syncthreads();
+    }
+    if (!refused && sum.y > 0) {  // pages that go back
+      ends[tid] = (int)incl.y;
+      __syncthreads();
+      for (int e = tid; e < (int)sum.y; e += kThreads) {
+        int lo = 0, hi = kThreads - 1;
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (ends[mid] > e) hi = mid; else lo = mid + 1;
+        }
+        const int in_head = e - (lo ? ends[lo - 1] : 0);
+        p.ring_out[(given + give_at + e) % c.n_pages] = p.table[(size_t)(at + lo) * c.max_pages + in_head];
+      }
+      __syncthreads();
+    }
+    take_at += sum.x;
+    give_at += sum.y;
+  }
+  cluster.sync();  // every CTA has read the counters and the others' sums
+  if (rank == 0 && tid == 0) {
+    p.counters_out[0] = refused ? taken : taken + take_all;
+    p.counters_out[1] = refused ? given : given + give_all;
+    if (refused && p.status)
+      atomicOr(p.status, (bad ? LAVA_DEV_BAD_ROWS : 0u) | (short_of ? LAVA_DEV_PAGES_EXHAUSTED : 0u));
+  }
+}
+
+lava_status launch_tables(const TableParams& p, cudaStream_t stream) {
+  // a CTA for every 1024 heads
+  int ctas = 1;
+  while (ctas < kMostCtas && ctas * kThreads < p.c.heads) ctas *= 2;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ctas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = ctas;
+  cfg.blockDim = kThreads;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, page_table_kernel, p);
+  count_launches(1);
+  return check_cuda(e, "page table launch");
+}
+
+}  // namespace
+}  // namespace lava
+
+using namespace lava;
+
+extern "C" {
+
+lava_status lava_page_admit(const lava_cache_desc* cache, int32_t first_seq, int32_t n_seqs,
+                            const int32_t* head_offsets, const int32_t* head_rows, int32_t* head_rows_out,
+                            int32_t* page_table, const int32_t* free_pages, const int64_t* counters,
+                            int64_t* counters_out, int32_t* first_row, uint32_t* status_word, void* stream) {
+  TableParams p = {};
+  const lava_status rc = make_cache(cache, &p.c);
+  if (rc != LAVA_OK) return rc;
+  if (!head_offsets || !head_rows || !head_rows_out || !page_table || !free_pages || !counters || !counters_out ||
+      !first_row)
+    return fail(LAVA_ERR_INVALID_ARG, "NULL argument");
+  if (n_seqs < 1 || first_seq < 0 || first_seq > p.c.batch - n_seqs)
+    return fail(LAVA_ERR_INVALID_ARG, "sequences %d ... %lld are not all in a cache of %d", first_seq,
+                (long long)first_seq + n_seqs - 1, p.c.batch);
+  p.head_offsets = head_offsets;
+  p.first_seq = first_seq;
+  p.n_seqs = n_seqs;
+  p.rows = head_rows;
+  p.rows_out = head_rows_out;
+  p.table = page_table;
+  p.ring = free_pages;
+  p.counters = (const long long*)counters;
+  p.counters_out = (long long*)counters_out;
+  p.first_row = first_row;
+  p.status = status_word;
+  return launch_tables(p, (cudaStream_t)stream);
+}
+
+lava_status lava_page_extend(const lava_cache_desc* cache, const int32_t* add, int32_t max_add,
+                             const int32_t* head_rows, int32_t* head_rows_out, int32_t* page_table,
+                             int32_t* free_pages, const int64_t* counters, int64_t* counters_out,
+                             int32_t* slots, uint32_t* status_word, void* stream) {
+  TableParams p = {};
+  const lava_status rc = make_cache(cache, &p.c);
+  if (rc != LAVA_OK) return rc;
+  if (!add || !head_rows || !head_rows_out || !page_table || !free_pages || !counters || !counters_out || !slots)
+    return fail(LAVA_ERR_INVALID_ARG, "NULL argument");
+  if (max_add < 1) return fail(LAVA_ERR_INVALID_ARG, "max_add must be >= 1");
+  p.add = add;
+  p.max_add = max_add;
+  p.rows = head_rows;
+  p.rows_out = head_rows_out;
+  p.table = page_table;
+  p.ring = free_pages;
+  p.ring_out = free_pages;
+  p.counters = (const long long*)counters;
+  p.counters_out = (long long*)counters_out;
+  p.slots = slots;
+  p.status = status_word;
+  return launch_tables(p, (cudaStream_t)stream);
+}
+
+}  // extern "C"
