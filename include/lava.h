@@ -401,8 +401,8 @@ typedef struct lava_cache_desc {
 
 /* Bytes of `workspace` for the paged calls of this cache: a status word (first 256 bytes, as in
  * lava_workspace_bytes), and what the attention's blocks exchange.  The caller zeroes it once after
- * allocating it; every call leaves it ready for the next.  Calls that may run at the same time need
- * a workspace each.  0 and lava_last_error() for an invalid descriptor. */
+ * allocating it (and after LAVA_DEV_WAIT_EXPIRED); every call leaves it ready for the next.  Calls that
+ * may run at the same time need a workspace each.  0 and lava_last_error() for an invalid descriptor. */
 LAVA_API size_t lava_cache_workspace_bytes(const lava_cache_desc* cache);
 
 /* Page tables from row counts.  Both take the pages that they need from the ring in the order of the

@@ -1,9 +1,26 @@
 // Attention of one new token over the pages of a paged cache.
 //
-// One block per (query head, layer and sequence), tiles of 1024 rows, fp32 throughout: logits in the base-2
-// domain, running maximum and sum, then the product with V.  Rows are read with 16-byte loads, d / 4 or d / 8
-// lanes per row.
+//     x_i = scale * q . K[i]  (capped: c tanh(x / c)),   out = sum_i e^(x_i - m) V[i] / sum_i e^(x_i - m)
+//
+// One pass over the rows with a running maximum m and sum, logits in the base-2 domain.  All query heads of a KV
+// head's group share the read of its rows.  What has to be read is the rows, once; everything else is small, so the
+// kernel is built to keep copies in flight:
+//
+// The tiles of all heads (64 rows; 32 of 512 bytes) form one line, which is cut into equal parts, one per CTA, two
+// CTAs per SM: heads of any lengths load all SMs alike.  Row counts live on the device, so every CTA finds its part
+// itself.  A producer warp walks the part: it looks up the tile's pages and has TMA fetch K and V in boxes of 16 rows
+// (the least page) into a ring of stages; boxes behind a head's last row are not fetched.  Four warps consume a
+// tile, a quarter of its rows each, with maxima and sums of their own until the head or the part ends; then they meet
+// through the memory of the last stage.  A head inside one part is finished there.  Of a head that continues in other
+// parts the partial result goes to memory; the CTA that comes last, as a counter tells, joins them in order.
+//
+// bf16: S = Q K^T and O += P V by mma.sync m16n8k16 (2 % of the tensor peak at the rate of HBM).  With up to 8 queries
+// the other 8 rows of the A operand are free: they carry what rounding the probabilities to bf16 left over, so the
+// products with V keep 16 bits of every probability at no cost; with 9 to 16 queries a second product does.  More
+// queries per KV head than 16 are taken 16 at a time.  fp32: a lane has a row (or a half or quarter of it) for the
+// logits, and some columns for the product with V; up to 8 queries at a time.
 #include <algorithm>
+#include <type_traits>
 
 #include <math.h>
 
@@ -14,123 +31,658 @@ namespace {
 
 using namespace sm100;
 
-constexpr int kThreads = 256;
-constexpr int kTile = 1024;
+constexpr int kConsumers = 4;                  // warps
+constexpr int kThreads = (kConsumers + 1) * 32;
+constexpr int kBoxRows = 16;
+constexpr int kCtasPerSm = 2;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+template <int D, bool BF16, int Q>
+struct Shape {
+  static constexpr int kRowBytes = D * (BF16 ? 2 : 4);
+  static constexpr int kTile = kRowBytes == 512 ? 32 : 64;       // rows
+  static constexpr int kWarpRows = kTile / kConsumers;
+  static constexpr int kBoxBytes = kBoxRows * kRowBytes;
+  static constexpr int kTileBytes = kTile * kRowBytes;
+  static constexpr int kStageBytes = 2 * kTileBytes;             // K, V
+  static constexpr int kStages = 96 * 1024 / kStageBytes;
+  static constexpr int kSmem = kStages * kStageBytes + 1024;     // (aligned to the swizzle's period inside)
+  static_assert(kConsumers * Q * D * 4 <= kStageBytes, "the warps' results fit a stage");
+};
 
 struct PageParams {
   Cache c;
-  int first_layer;
+  int first_head;          // of the call's first layer
+  int heads;               // of the call's layers
+  int subs, per_sub;       // a group's queries are taken in `subs` portions of `per_sub`
   const void* q;           // [layers, batch, H_q, d]
-  const char* k_pages;
-  const char* v_pages;
   const int* table;
   const int* rows;
   void* out;
   float* lse;
+  float* part;             // [CTA][2][Q][D]: partial results of the part's first and last head,
+  float2* part_ml;         // [CTA][2][Q]: the maximum that they are relative to, and the sum
+  int* counters;           // [CTA]: parts that have left their result of the head that begins last in CTA's part
+  unsigned* status;
+  long long wait_cycles;
 };
 
-template <int D, bool BF16>
-__global__ void __launch_bounds__(kThreads)
-decode_pages_kernel(const PageParams p) {
-  in_stream_order();
-  constexpr int kPer = BF16 ? 8 : 4;  // elements per 16-byte load
-  constexpr int kLanes = D / kPer;    // lanes per row
-  constexpr int kGroups = kThreads / kLanes;
-  __shared__ float pr[kTile], red[8];
-  __shared__ float sums[kGroups][D];
-  const Cache& c = p.c;
-  const int h = blockIdx.x, prob = blockIdx.y;
-  const size_t head = ((size_t)p.first_layer * c.batch + prob) * c.n_kv_heads + h / c.group;
-  const int len = (int)min((long long)max(0, p.rows[head]), (long long)c.max_pages << c.page_shift);
-  const int* pages = p.table + head * c.max_pages;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, group = tid / kLanes, col = tid % kLanes;
-  auto unpack = [](const uint4& raw, float (&x)[kPer]) {
-    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+struct Ctl {
+  volatile int abort_flag;
+  long long wait_cycles;
+};
+
+struct Start {
+  int head, sub, tile;  // head of the call, portion of its queries, tile
+};
+
+template <class S>
+__device__ __forceinline__ int tiles_of(int len) {
+  return (len + S::kTile - 1) / S::kTile;
+}
+__device__ __forceinline__ int head_len(const PageParams& p, int h) {
+  return min(max(0, p.rows[p.first_head + h]), p.c.max_pages << p.c.page_shift);
+}
+
+// Byte address of 16-byte piece c of row r in a tile: boxes of 16 rows, in them blocks of 128 bytes of every row
+// with the 128-byte swizzle.
+template <class S>
+__device__ __forceinline__ uint32_t piece_at(uint32_t tile, int r, int c) {
+  return tile + (r >> 4) * S::kBoxBytes + (c >> 3) * (kBoxRows * 128) + (r & 15) * 128 + (((c ^ r) & 7) << 4);
+}
+
+// The logit in the base-2 domain of a product of q and a row.
+struct Logit {
+  float scale, in, cap;  // scale * log2(e); or, capped: scale / cap, cap * log2(e)
+  __device__ explicit Logit(const Cache& c)
+      : scale(c.scale * kLog2e), in(c.softcap > 0.f ? c.scale / c.softcap : 0.f), cap(c.softcap * kLog2e) {}
+  __device__ __forceinline__ float of(float s) const {
+    if (cap == 0.f) return s * scale;
+    // tanh z = 1 - 2 / (e^(2 z) + 1); near zero, where that cancels, its series (to z^9: 2e-9 at 1/4)
+    const float z = s * in, zz = z * z;
+    const float t = 1.f - __fdividef(2.f, fast_exp2(z * (2.f * kLog2e)) + 1.f);
+    const float series = z * fmaf(zz, fmaf(zz, fmaf(zz, fmaf(zz, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+    return cap * (fabsf(z) < 0.25f ? series : t);
+  }
+};
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float bf16_lo(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+__device__ __forceinline__ void ldmatrix_x4(uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3, uint32_t saddr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3)
+               : "r"(saddr)
+               : "memory");
+}
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// barrier of the consumer warps; whether `x` holds in all their threads
+__device__ __forceinline__ bool meet_all(bool x) {
+  uint32_t y;
+  asm volatile(
+      "{\n.reg .pred p, q;\nsetp.ne.u32 q, %1, 0;\nbarrier.cta.red.and.pred p, 1, 128, q;\nselp.u32 %0, 1, 0, p;\n}"
+      : "=r"(y) : "r"((uint32_t)x) : "memory");
+  return y != 0;
+}
+static_assert(kConsumers * 32 == 128, "meet_all");
+__device__ __forceinline__ void meet() { named_bar_sync(1, kConsumers * 32); }
+// what exponentials are taken against: 0 where there is no logit above -infinity
+__device__ __forceinline__ float finite_ref(float m) { return m == -INFINITY ? 0.f : m; }
+
+// largest logit of query q that the warps have met
+template <int Q>
+__device__ __forceinline__ float top_of(const float2 (*stats)[Q], int q) {
+  float top = stats[0][q].x;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if constexpr (BF16) {
-        x[2 * j] = __uint_as_float(w[j] << 16);
-        x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+  for (int i = 1; i < kConsumers; ++i) top = fmaxf(top, stats[i][q].x);
+  return top;
+}
+
+// ---- bf16: tensor cores ----------------------------------------------------------------------------
+// Thread (g = lane / 4, t = lane % 4) has query row g, and with 16 queries g + 8 too.
+template <int D, int Q>
+struct TensorWarp {
+  using S = Shape<D, true, Q>;
+  static constexpr int kRowsOf = Q / 8;
+  uint32_t qa[D / 16][2 * kRowsOf];
+  float m[kRowsOf], l[kRowsOf], o[D / 8][4];
+
+  __device__ __forceinline__ void begin(const PageParams& p, size_t q_row, int queries) {
+    const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+#pragma unroll
+    for (int u = 0; u < kRowsOf; ++u) {
+      const bool there = g + 8 * u < queries;
+      const uint32_t* qh = reinterpret_cast<const uint32_t*>(p.q) + (q_row + g + 8 * u) * (D / 2);
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) {
+        qa[s][u] = there ? qh[8 * s + t] : 0u;
+        qa[s][kRowsOf + u] = there ? qh[8 * s + 4 + t] : 0u;
+      }
+      m[u] = -INFINITY;
+      l[u] = 0.f;
+    }
+#pragma unroll
+    for (int nd = 0; nd < D / 8; ++nd) o[nd][0] = o[nd][1] = o[nd][2] = o[nd][3] = 0.f;
+  }
+
+  // rows r0 ... r0 + 15 of the tile, of which `valid` (> 0) are there; v_ready() waits for V
+  template <class Wait>
+  __device__ __forceinline__ bool tile(uint32_t k_tile, uint32_t v_tile, int r0, int valid, const Logit& logit, float*,
+                                       Wait v_ready) {
+    const int lane = threadIdx.x & 31, t = lane & 3, mi = lane >> 3, r8 = lane & 7;
+    float s[2][4] = {};
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {  // matrices (keys 0-7, piece 2 ks), (0-7, 2 ks + 1), (8-15, ...)
+      uint32_t b0, b1, b2, b3;
+      ldmatrix_x4(b0, b1, b2, b3, piece_at<S>(k_tile, r0 + (mi >> 1) * 8 + r8, 2 * ks + (mi & 1)));
+      const uint32_t a0 = qa[ks][0], a1 = kRowsOf == 2 ? qa[ks][1] : 0u;
+      const uint32_t a2 = qa[ks][kRowsOf], a3 = kRowsOf == 2 ? qa[ks][kRowsOf + 1] : 0u;
+      mma_bf16_16816(s[0][0], s[0][1], s[0][2], s[0][3], a0, a1, a2, a3, b0, b1);
+      mma_bf16_16816(s[1][0], s[1][1], s[1][2], s[1][3], a0, a1, a2, a3, b2, b3);
+    }
+    uint32_t hi[2][kRowsOf], lo[2][kRowsOf];  // [keys 0-7, 8-15][row]
+    float corr[kRowsOf];
+    bool moved = false;
+#pragma unroll
+    for (int u = 0; u < kRowsOf; ++u) {
+      float x[2][2], best = -INFINITY;
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          x[n][e] = 8 * n + 2 * t + e < valid ? logit.of(s[n][2 * u + e]) : -INFINITY;
+          best = fmaxf(best, x[n][e]);
+        }
+      best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
+      best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 2));
+      const float m_new = fmaxf(m[u], best), ref = finite_ref(m_new);
+      corr[u] = fast_exp2(m[u] - ref);
+      moved |= m_new != m[u];
+      m[u] = m_new;
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        x[n][0] = fast_exp2(x[n][0] - ref);
+        x[n][1] = fast_exp2(x[n][1] - ref);
+        hi[n][u] = pack_bf16(x[n][0], x[n][1]);
+        lo[n][u] = pack_bf16(x[n][0] - bf16_lo(hi[n][u]), x[n][1] - bf16_hi(hi[n][u]));
+      }
+      l[u] = fmaf(l[u], corr[u], (x[0][0] + x[0][1]) + (x[1][0] + x[1][1]));
+    }
+    if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+      for (int nd = 0; nd < D / 8; ++nd)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[nd][e] *= corr[kRowsOf == 2 ? e >> 1 : 0];
+    }
+    if (!v_ready()) return false;
+    if (valid < 16) {  // rows behind the last one may hold anything: their probabilities are 0, so must they be
+      for (int i = lane; i < (16 - valid) * (D / 8); i += 32)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(piece_at<S>(v_tile, r0 + valid + i / (D / 8), i % (D / 8))),
+                     "r"(0) : "memory");
+      fence_async_proxy();  // (before the next copy into this stage)
+      __syncwarp();
+    }
+#pragma unroll
+    for (int nd = 0; nd < D / 8; nd += 2) {
+      uint32_t b0, b1, b2, b3;
+      ldmatrix_x4_trans(b0, b1, b2, b3, piece_at<S>(v_tile, r0 + (mi & 1) * 8 + r8, nd + (mi >> 1)));
+      if constexpr (kRowsOf == 1) {
+        mma_bf16_16816(o[nd][0], o[nd][1], o[nd][2], o[nd][3], hi[0][0], lo[0][0], hi[1][0], lo[1][0], b0, b1);
+        mma_bf16_16816(o[nd + 1][0], o[nd + 1][1], o[nd + 1][2], o[nd + 1][3], hi[0][0], lo[0][0], hi[1][0], lo[1][0], b2, b3);
       } else {
-        x[j] = __uint_as_float(w[j]);
+        mma_bf16_16816(o[nd][0], o[nd][1], o[nd][2], o[nd][3], lo[0][0], lo[0][1], lo[1][0], lo[1][1], b0, b1);
+        mma_bf16_16816(o[nd + 1][0], o[nd + 1][1], o[nd + 1][2], o[nd + 1][3], lo[0][0], lo[0][1], lo[1][0], lo[1][1], b2, b3);
+        mma_bf16_16816(o[nd][0], o[nd][1], o[nd][2], o[nd][3], hi[0][0], hi[0][1], hi[1][0], hi[1][1], b0, b1);
+        mma_bf16_16816(o[nd + 1][0], o[nd + 1][1], o[nd + 1][2], o[nd + 1][3], hi[0][0], hi[0][1], hi[1][0], hi[1][1], b2, b3);
       }
     }
-  };
-  auto row_piece = [&](const char* pool, int row) {  // zeros where the page is none of the pool
-    const int page = pages[row >> c.page_shift];
-    if ((unsigned)page >= (unsigned)c.n_pages) return uint4{};
-    const long long at = ((long long)page << c.page_shift) + (row & (c.page_rows - 1));
-    return reinterpret_cast<const uint4*>(pool)[at * kLanes + col];
-  };
-  auto block_reduce = [&](float x, auto op) {  // the same order in every thread
-    for (int o = 16; o > 0; o >>= 1) x = op(x, __shfl_xor_sync(0xffffffffu, x, o));
-    __syncthreads();
-    if (lane == 0) red[warp] = x;
-    __syncthreads();
-    x = red[0];
-    for (int w = 1; w < kThreads / 32; ++w) x = op(x, red[w]);
-    return x;
-  };
-  float q[kPer];
-  unpack(reinterpret_cast<const uint4*>(p.q)[((long long)prob * c.n_q_heads + h) * kLanes + col], q);
-  float m = -INFINITY, l = 0.f, acc[kPer] = {};
-  for (int i0 = 0; i0 < len; i0 += kTile) {
-    const int cnt = min(kTile, len - i0);
-    float best = -INFINITY;
-    for (int r0 = 0; r0 < cnt; r0 += kGroups) {
-      const int r = r0 + group;
-      float x[kPer], z = 0.f;
-      unpack(r < cnt ? row_piece(p.k_pages, i0 + r) : uint4{}, x);
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) z = fmaf(q[j], x[j], z);
-      for (int o = kLanes / 2; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-      z *= c.scale;
-      if (c.softcap > 0.f) z = c.softcap * tanhf(z / c.softcap);
-      z *= kLog2e;
-      if (r < cnt) {
-        best = fmaxf(best, z);
-        if (col == 0) pr[r] = z;
-      }
-    }
-    const float m_new = fmaxf(m, block_reduce(best, [](float a, float b) { return fmaxf(a, b); }));
-    float sum = 0.f;
-    for (int r = tid; r < cnt; r += kThreads) {
-      const float e = exp2f(pr[r] - m_new);
-      pr[r] = e;
-      sum += e;
-    }
-    sum = block_reduce(sum, [](float a, float b) { return a + b; });  // also: all of pr is written
-    const float corr = exp2f(m - m_new);
-    l = l * corr + sum;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) acc[j] *= corr;
-    m = m_new;
-    for (int r = group; r < cnt; r += kGroups) {
-      float x[kPer];
-      unpack(row_piece(p.v_pages, i0 + r), x);
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) acc[j] = fmaf(pr[r], x[j], acc[j]);
-    }
-    __syncthreads();  // pr is written again
+    return true;
   }
+
+  __device__ __forceinline__ void leave_stats(float2* ml) {  // [Q] of this warp
+    const int g = (threadIdx.x & 31) >> 2;
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) sums[group][col * kPer + j] = acc[j];
+    for (int u = 0; u < kRowsOf; ++u) {
+      l[u] += __shfl_xor_sync(0xffffffffu, l[u], 1);
+      l[u] += __shfl_xor_sync(0xffffffffu, l[u], 2);
+      if ((threadIdx.x & 3) == 0) ml[g + 8 * u] = make_float2(m[u], l[u]);
+    }
+  }
+  // column `col` of query q lies at float `col ^ swizzle(q)` of its row (spreads the rows over the banks)
+  static __device__ __forceinline__ int swizzle(int q) { return (q & 7) * 8; }
+  __device__ __forceinline__ void leave_sums(float* to, const float2 (*stats)[Q]) {  // [Q][D] of this warp
+    const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+#pragma unroll
+    for (int u = 0; u < kRowsOf; ++u) {
+      const int q = g + 8 * u;
+      const float c = fast_exp2(m[u] - finite_ref(top_of<Q>(stats, q)));
+#pragma unroll
+      for (int nd = 0; nd < D / 8; ++nd) {
+        const float a = kRowsOf == 2 ? o[nd][2 * u] : o[nd][0] + o[nd][2], b = kRowsOf == 2 ? o[nd][2 * u + 1] : o[nd][1] + o[nd][3];
+        *reinterpret_cast<float2*>(to + q * D + ((nd * 8 + 2 * t) ^ swizzle(q))) = make_float2(a * c, b * c);
+      }
+    }
+  }
+};
+
+// ---- fp32 ------------------------------------------------------------------------------------------
+// A warp has kWarpRows rows of a tile: for the logits lane % kWarpRows is the row and the lanes that share it split
+// its pieces; for the product with V a lane has D / 32 columns.
+template <int D, int Q>
+struct PlainWarp {
+  using S = Shape<D, false, Q>;
+  static constexpr int kRows = S::kWarpRows, kSplit = 32 / kRows, kPieces = D / 4 / kSplit, kCols = D / 32;
+  const float* qs;        // [Q][D] in shared memory
+  float m[Q], l[Q], o[Q][kCols];
+
+  __device__ __forceinline__ void begin(const PageParams& p, size_t q_row, int queries, float* q_mem) {
+    // (all warps are through with the queries before: they have met)
+    for (int i = threadIdx.x; i < Q * (D / 4); i += kConsumers * 32)
+      reinterpret_cast<float4*>(q_mem)[i] = i / (D / 4) < queries
+          ? reinterpret_cast<const float4*>(p.q)[q_row * (D / 4) + i] : make_float4(0.f, 0.f, 0.f, 0.f);
+    meet();
+    qs = q_mem;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      m[q] = -INFINITY;
+      l[q] = 0.f;
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) o[q][c] = 0.f;
+    }
+  }
+
+  template <class Wait>
+  __device__ __forceinline__ bool tile(uint32_t k_tile, uint32_t v_tile, int r0, int valid, const Logit& logit,
+                                       float* probs, Wait v_ready) {
+    const int lane = threadIdx.x & 31, row = lane % kRows, share = lane / kRows;
+    float z[Q] = {};
+#pragma unroll 4
+    for (int i = 0; i < kPieces; ++i) {
+      const int c = share * kPieces + i;
+      float4 k;
+      asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w)
+                   : "r"(piece_at<S>(k_tile, r0 + row, c)));
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const float4 a = *reinterpret_cast<const float4*>(qs + q * D + 4 * c);
+        z[q] = fmaf(a.x, k.x, fmaf(a.y, k.y, fmaf(a.z, k.z, fmaf(a.w, k.w, z[q]))));
+      }
+    }
+    float corr[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+#pragma unroll
+      for (int w = kRows; w < 32; w *= 2) z[q] += __shfl_xor_sync(0xffffffffu, z[q], w);
+      z[q] = row < valid ? logit.of(z[q]) : -INFINITY;
+      float best = z[q];
+#pragma unroll
+      for (int w = 1; w < kRows; w *= 2) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, w));
+      const float m_new = fmaxf(m[q], best), ref = finite_ref(m_new);
+      corr[q] = fast_exp2(m[q] - ref);
+      m[q] = m_new;
+      z[q] = fast_exp2(z[q] - ref);
+      l[q] = l[q] * corr[q] + (share == 0 ? z[q] : 0.f);  // a lane's own rows
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) o[q][c] *= corr[q];
+    }
+    __syncwarp();  // (the probabilities of the tile before have been read)
+    if (share == 0)
+#pragma unroll
+      for (int q = 0; q < Q; q += 4)
+        *reinterpret_cast<float4*>(probs + row * Q + q) = make_float4(z[q], z[q + 1], z[q + 2], z[q + 3]);
+    __syncwarp();
+    if (!v_ready()) return false;
+#pragma unroll 4
+    for (int r = 0; r < kRows; ++r) {
+      if (r >= valid) break;  // rows behind the last one may hold anything
+      float v[kCols];
+      if constexpr (kCols == 4)
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3])
+                     : "r"(piece_at<S>(v_tile, r0 + r, lane)));
+      else
+        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1])
+                     : "r"(piece_at<S>(v_tile, r0 + r, lane / 2) + (lane & 1) * 8));
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const float pr = probs[r * Q + q];
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) o[q][c] = fmaf(pr, v[c], o[q][c]);
+      }
+    }
+    return true;
+  }
+
+  __device__ __forceinline__ void leave_stats(float2* ml) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+#pragma unroll
+      for (int w = 16; w > 0; w >>= 1) l[q] += __shfl_xor_sync(0xffffffffu, l[q], w);
+      if ((threadIdx.x & 31) == 0) ml[q] = make_float2(m[q], l[q]);
+    }
+  }
+  static __device__ __forceinline__ int swizzle(int) { return 0; }
+  __device__ __forceinline__ void leave_sums(float* to, const float2 (*stats)[Q]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const float c = fast_exp2(m[q] - finite_ref(top_of<Q>(stats, q)));
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) to[q * D + lane * kCols + j] = o[q][j] * c;
+    }
+  }
+};
+
+template <bool BF16>
+__device__ __forceinline__ void store4(void* out, size_t at, float4 x) {  // `at`: first of four elements
+  if constexpr (BF16)
+    *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(out) + at) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+  else
+    *reinterpret_cast<float4*>(reinterpret_cast<float*>(out) + at) = x;
+}
+
+// The partial results of `n` parts of a head, from CTA `w0` on (there the last of its part, then the first ones),
+// joined in order: a warp per query.
+template <int D, bool BF16, int Q>
+__device__ __forceinline__ void join_parts(const PageParams& p, int w0, int n, int queries, size_t q_row) {
+  constexpr int kCols = D / 32, kAhead = 8;
+  using Cols = typename std::conditional<D == 128, float4, float2>::type;
+  const int lane = threadIdx.x & 31;
+  auto slot = [&](int i) { return (size_t)(w0 + i) * 2 + (i == 0); };
+  for (int q = threadIdx.x >> 5; q < queries; q += kConsumers) {
+    float top = -INFINITY;
+    for (int i = lane; i < n; i += 32) top = fmaxf(top, __ldcg(p.part_ml + slot(i) * Q + q).x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float ref = finite_ref(top);
+    float acc[kCols] = {}, l = 0.f;
+    for (int s0 = 0; s0 < n; s0 += 32) {
+      const float2 ml = s0 + lane < n ? __ldcg(p.part_ml + slot(s0 + lane) * Q + q) : make_float2(-INFINITY, 0.f);
+      const float w = fast_exp2(ml.x - ref);
+      const int end = min(32, n - s0);
+      for (int i0 = 0; i0 < end; i0 += kAhead) {
+        Cols v[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+          if (i0 + j < end) v[j] = __ldcg(reinterpret_cast<const Cols*>(p.part + (slot(s0 + i0 + j) * Q + q) * D) + lane);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          if (i0 + j >= end) break;
+          const float wi = __shfl_sync(0xffffffffu, w, i0 + j);
+          const float* f = reinterpret_cast<const float*>(&v[j]);
+#pragma unroll
+          for (int c = 0; c < kCols; ++c) acc[c] = fmaf(wi, f[c], acc[c]);
+          l = fmaf(wi, __shfl_sync(0xffffffffu, ml.y, i0 + j), l);
+        }
+      }
+    }
+    const size_t at = (q_row + q) * D + lane * kCols;
+    if constexpr (D == 128) {
+      store4<BF16>(p.out, at, make_float4(acc[0] / l, acc[1] / l, acc[2] / l, acc[3] / l));
+    } else if constexpr (BF16) {
+      *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.out) + at) = pack_bf16(acc[0] / l, acc[1] / l);
+    } else {
+      *reinterpret_cast<float2*>(reinterpret_cast<float*>(p.out) + at) = make_float2(acc[0] / l, acc[1] / l);
+    }
+    if (p.lse && lane == 0) p.lse[q_row + q] = (top + fast_log2(l)) * kLn2;
+  }
+}
+
+template <int D, bool BF16, int Q>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                    const __grid_constant__ PageParams p) {
+  using S = Shape<D, BF16, Q>;
+  using Warp = typename std::conditional<BF16, TensorWarp<D, Q>, PlainWarp<D, Q>>::type;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) uint64_t full_k[S::kStages], full_v[S::kStages], empty[S::kStages];
+  __shared__ Ctl ctl;
+  __shared__ int issued, last_one;
+  __shared__ Start start;
+  __shared__ float2 stats[kConsumers][Q];
+  __shared__ __align__(16) float q_mem[BF16 ? 4 : Q * D];  // fp32: the queries
+  __shared__ __align__(16) float prob_mem[BF16 ? 4 : kConsumers * S::kWarpRows * Q];
+  const Cache& c = p.c;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+
+  if (tid == 0) {
+    for (int s = 0; s < S::kStages; ++s) {
+      mbar_init(smem_u32(&full_k[s]), 1);
+      mbar_init(smem_u32(&full_v[s]), 1);
+      mbar_init(smem_u32(&empty[s]), kConsumers);
+    }
+    ctl.abort_flag = 0;
+    ctl.wait_cycles = p.wait_cycles;
+    issued = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  in_stream_order();
+
+  // ---- this CTA's part of the line of all tiles -----------------------------------------------------
+  long long total, at0, at1;
+  int parts;
+  {
+    const int share = (p.heads + kThreads - 1) / kThreads;
+    const int h0 = min(p.heads, tid * share), h1 = min(p.heads, h0 + share);
+    int tiles = 0;
+#pragma unroll 4
+    for (int h = h0; h < h1; ++h) {
+      const int len = head_len(p, h);
+      tiles += tiles_of<S>(len);
+      if (len == 0 && h % (int)gridDim.x == (int)blockIdx.x) {  // no rows: zeros
+        const int prob = h / c.n_kv_heads, kvh = h - prob * c.n_kv_heads;
+        const size_t row = (size_t)prob * c.n_q_heads + (size_t)kvh * c.group;
+        for (int i = 0; i < c.group * D; i += 4) store4<BF16>(p.out, row * D + i, make_float4(0.f, 0.f, 0.f, 0.f));
+        if (p.lse)
+          for (int i = 0; i < c.group; ++i) p.lse[row + i] = -INFINITY;
+      }
+    }
+    // (a head has 2^26 tiles at most, all heads of a pool without shared pages fewer; sums are kept in 64 bits)
+    long long incl = tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += y;
+    }
+    __shared__ long long sums[kThreads / 32];
+    if (lane == 31) sums[warp] = incl;
+    __syncthreads();
+    long long before = incl - tiles, all = 0;
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) before += sums[w];
+      all += sums[w];
+    }
+    total = all * p.subs;
+    parts = (int)min((long long)gridDim.x, total);
+    if ((int)blockIdx.x >= parts) return;
+    at0 = total * blockIdx.x / parts;
+    at1 = total * (blockIdx.x + 1) / parts;
+    before *= p.subs;
+    if (at0 >= before && at0 < before + (long long)tiles * p.subs) {
+      int h = h0, n = tiles_of<S>(head_len(p, h));
+      long long at = before;
+      while (at + (long long)n * p.subs <= at0) {
+        at += (long long)n * p.subs;
+        n = tiles_of<S>(head_len(p, ++h));
+      }
+      start = {h, (int)((at0 - at) / n), (int)((at0 - at) % n)};
+    }
+    __syncthreads();
+  }
+  long long left = at1 - at0;
+  int sub = start.sub, t0 = start.tile;  // of the head in hand; 0 in the heads that follow
+  int stage = 0, use = 0;
+  bool alive = true;
+  const auto wait = [&](uint64_t* bar, int parity) {  // the same in all lanes
+    return __all_sync(0xffffffffu, wait_bar(smem_u32(bar), parity, &ctl, p.status)) != 0;
+  };
+  const auto next_stage = [&] {
+    if (++stage == S::kStages) {
+      stage = 0;
+      ++use;
+    }
+  };
+
+  if (warp == kConsumers) {
+    // ---- producer ----------------------------------------------------------------------------------
+    for (int h = start.head; left > 0 && alive; ++h, sub = 0) {
+      const int len = head_len(p, h), n = tiles_of<S>(len);
+      if (n == 0) continue;
+      const int* pages = p.table + (size_t)(p.first_head + h) * c.max_pages;
+      for (; sub < p.subs && left > 0 && alive; ++sub, t0 = 0) {
+        const int t1 = (int)min((long long)n, t0 + left);
+        left -= t1 - t0;
+        for (int t = t0; t < t1; ++t) {
+          const int row0 = t * S::kTile;
+          const int boxes = min(S::kTile / kBoxRows, (len - row0 + kBoxRows - 1) / kBoxRows);
+          // lane 2 i + v: box i of K or V
+          const int row = row0 + (lane >> 1) * kBoxRows;
+          int at = 0;
+          if (lane < 2 * boxes) {
+            const int page = pages[row >> c.page_shift];
+            // (a page that is none of the pool: behind the pool's rows, where copies give zeros)
+            at = (unsigned)page < (unsigned)c.n_pages ? (page << c.page_shift) + (row & (c.page_rows - 1))
+                                                      : c.n_pages << c.page_shift;
+          }
+          if (use > 0) alive = wait(&empty[stage], (use - 1) & 1);
+          if (!alive) break;
+          const uint32_t k_tile = ring + stage * S::kStageBytes;
+          if (lane == 0) {
+            mbar_expect_tx(smem_u32(&full_k[stage]), boxes * S::kBoxBytes);
+            mbar_expect_tx(smem_u32(&full_v[stage]), boxes * S::kBoxBytes);
+            ++issued;
+          }
+          __syncwarp();
+          if (lane < 2 * boxes) {
+            const bool v = lane & 1;
+            tma_load_3d(k_tile + (v ? S::kTileBytes : 0) + (lane >> 1) * S::kBoxBytes, v ? &map_v : &map_k, 0, at, 0,
+                        smem_u32(v ? &full_v[stage] : &full_k[stage]));
+          }
+          next_stage();
+        }
+      }
+    }
+  } else {
+    // ---- consumers ---------------------------------------------------------------------------------
+    Warp w;
+    const Logit logit(c);
+    float* const probs = prob_mem + (BF16 ? 0 : warp * S::kWarpRows * Q);
+    long long at = at0 - t0;  // first tile of the head's portion on the line
+    for (int h = start.head; left > 0 && alive; ++h, sub = 0) {
+      const int len = head_len(p, h), n = tiles_of<S>(len);
+      if (n == 0) continue;
+      const int prob = h / c.n_kv_heads, kvh = h - prob * c.n_kv_heads;
+      for (; sub < p.subs && left > 0; ++sub, t0 = 0) {
+        const int t1 = (int)min((long long)n, t0 + left);
+        const int queries = min(p.per_sub, c.group - sub * p.per_sub);
+        const size_t q_row = (size_t)prob * c.n_q_heads + (size_t)kvh * c.group + sub * p.per_sub;
+        if constexpr (BF16) w.begin(p, q_row, queries);
+        else w.begin(p, q_row, queries, q_mem);
+        for (int t = t0; t < t1; ++t) {
+          const uint32_t k_tile = ring + stage * S::kStageBytes, v_tile = k_tile + S::kTileBytes;
+          const int r0 = warp * S::kWarpRows, valid = min(S::kWarpRows, len - t * S::kTile - r0);
+          alive = wait(&full_k[stage], use & 1);
+          const auto v_ready = [&] { return wait(&full_v[stage], use & 1); };
+          if (alive) alive = valid > 0 ? w.tile(k_tile, v_tile, r0, valid, logit, probs, v_ready) : v_ready();
+          if (!alive) break;
+          if (t + 1 < t1) {  // (the last stage is kept for the meeting)
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
+            next_stage();
+          }
+        }
+        // the warps meet: maxima and sums, then the sums of V against the common maximum
+        w.leave_stats(stats[warp]);
+        alive = meet_all(alive);
+        if (!alive) break;
+        float* const room = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)) + stage * S::kStageBytes);
+        w.leave_sums(room + warp * Q * D, stats);
+        meet();
+        const bool whole = t0 == 0 && t1 == n;
+        const size_t slot = (size_t)blockIdx.x * 2 + (t0 == 0);
+        for (int e = tid; e < queries * (D / 4); e += kConsumers * 32) {
+          const int q = e / (D / 4), col = e % (D / 4) * 4;
+          const float top = top_of<Q>(stats, q);
+          float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+          float l = 0.f;
+#pragma unroll
+          for (int i = 0; i < kConsumers; ++i) {
+            const float4 f = *reinterpret_cast<const float4*>(room + (i * Q + q) * D + (col ^ Warp::swizzle(q)));
+            a = make_float4(a.x + f.x, a.y + f.y, a.z + f.z, a.w + f.w);
+            l = fmaf(stats[i][q].y, fast_exp2(stats[i][q].x - finite_ref(top)), l);
+          }
+          if (whole) {
+            store4<BF16>(p.out, (q_row + q) * D + col, make_float4(a.x / l, a.y / l, a.z / l, a.w / l));
+            if (p.lse && col == 0) p.lse[q_row + q] = (top + fast_log2(l)) * kLn2;
+          } else {
+            *reinterpret_cast<float4*>(p.part + (slot * Q + q) * D + col) = a;
+            if (col == 0) p.part_ml[slot * Q + q] = make_float2(top, l);
+          }
+        }
+        fence_async_proxy();  // (the room was written; the next copy into this stage comes after)
+        if (!whole) __threadfence();
+        meet();
+        if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
+        next_stage();
+        if (!whole) {
+          // the parts that the portion's tiles `at` ... `at + n - 1` of the line lie in
+          const int w0 = (int)(((at + 1) * parts - 1) / total), w1 = (int)(((at + n) * parts - 1) / total);
+          if (tid == 0) last_one = atomicAdd(p.counters + w0, 1) == w1 - w0;
+          meet();
+          if (last_one) {
+            __threadfence();
+            join_parts<D, BF16, Q>(p, w0, w1 - w0 + 1, queries, q_row);
+            if (tid == 0) p.counters[w0] = 0;
+          }
+          meet();  // (last_one is written again)
+        }
+        left -= t1 - t0;
+        at += n;
+      }
+    }
+  }
+  // after a wait that gave up: no CTA leaves under a copy of its own
   __syncthreads();
-  const size_t at = (size_t)prob * c.n_q_heads + h;
-  if (tid < D) {
-    float x = 0.f;
-    for (int i = 0; i < kGroups; ++i) x += sums[i][tid];
-    x = len > 0 ? x / l : 0.f;
-    if constexpr (BF16)
-      reinterpret_cast<__nv_bfloat16*>(p.out)[at * D + tid] = __float2bfloat16_rn(x);
-    else
-      reinterpret_cast<float*>(p.out)[at * D + tid] = x;
+  if (ctl.abort_flag && tid == 0) {
+    for (int i = max(0, issued - S::kStages); i < issued; ++i) {
+      wait_bar(smem_u32(&full_k[i % S::kStages]), (i / S::kStages) & 1, &ctl, p.status, false);
+      wait_bar(smem_u32(&full_v[i % S::kStages]), (i / S::kStages) & 1, &ctl, p.status, false);
+    }
   }
-  if (p.lse && tid == 0) p.lse[at] = len > 0 ? (m + log2f(l)) * kLn2 : -INFINITY;
+}
+
+// A group's queries in portions that a warp can hold.
+struct Portions {
+  int held, subs, per_sub;
+};
+Portions portions_of(const Cache& c) {
+  const int most = c.dtype == LAVA_BF16 ? 16 : 8;
+  const int subs = (c.group + most - 1) / most, per_sub = (c.group + subs - 1) / subs;
+  return {per_sub <= most / 2 ? most / 2 : most, subs, per_sub};
 }
 
 constexpr size_t kStatusBytes = 256;
+int most_ctas() { return kCtasPerSm * (sm_count() > 0 ? sm_count() : 148); }
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+size_t counter_bytes() { return up256(most_ctas() * sizeof(int)); }
+size_t slots_of(const Cache& c) { return (size_t)most_ctas() * 2 * portions_of(c).held; }
+
+template <int D, bool BF16, int Q>
+lava_status launch(const CUtensorMap& map_k, const CUtensorMap& map_v, PageParams& p, cudaStream_t stream) {
+  using S = Shape<D, BF16, Q>;
+  const auto kernel = decode_pages_kernel<D, BF16, Q>;
+  const lava_status rc = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem),
+                                    "paged decode attention attribute");
+  if (rc != LAVA_OK) return rc;
+  const long long most = ((((long long)p.c.max_pages << p.c.page_shift) + S::kTile - 1) / S::kTile) * p.heads * p.subs;
+  const int grid = (int)std::min<long long>(most_ctas(), most);
+  const cudaError_t e = launch_in_order(kernel, grid, kThreads, S::kSmem, stream, map_k, map_v, p);
+  count_launches(1);
+  return check_cuda(e, "paged decode attention launch");
+}
 
 }  // namespace
 }  // namespace lava
@@ -141,15 +693,17 @@ extern "C" {
 
 size_t lava_cache_workspace_bytes(const lava_cache_desc* cache) {
   Cache c;
-  return make_cache(cache, &c) == LAVA_OK ? kStatusBytes : 0;
+  if (make_cache(cache, &c) != LAVA_OK) return 0;
+  return kStatusBytes + counter_bytes() + up256(slots_of(c) * c.head_dim * sizeof(float)) +
+         up256(slots_of(c) * sizeof(float2));
 }
 
 lava_status lava_decode_attention_pages(const lava_cache_desc* cache, int32_t first_layer, int32_t n_layers,
                                         const void* q, const void* k_pages, const void* v_pages,
                                         const int32_t* page_table, const int32_t* head_rows, void* out, float* lse,
                                         void* workspace, size_t workspace_bytes, void* stream) {
-  PageParams p;
-  const lava_status rc = make_cache(cache, &p.c);
+  PageParams p = {};
+  lava_status rc = make_cache(cache, &p.c);
   if (rc != LAVA_OK) return rc;
   const Cache& c = p.c;
   if (n_layers < 1 || first_layer < 0 || first_layer > c.n_layers - n_layers)
@@ -159,27 +713,39 @@ lava_status lava_decode_attention_pages(const lava_cache_desc* cache, int32_t fi
     return fail(LAVA_ERR_INVALID_ARG, "NULL argument");
   if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out))
     return fail(LAVA_ERR_INVALID_ARG, "q, k_pages, v_pages and out must be 16-byte aligned");
-  if ((long long)n_layers * c.batch > 65535)
-    return fail(LAVA_ERR_UNSUPPORTED, "n_layers*batch must be <= 65535");
   const size_t need = lava_cache_workspace_bytes(cache);
   if (!workspace || workspace_bytes < need)
     return fail(LAVA_ERR_WORKSPACE, "workspace too small: %zu < %zu bytes", workspace_bytes, need);
   if (!aligned16(workspace)) return fail(LAVA_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
-  p.first_layer = first_layer;
+  CUtensorMap map_k, map_v;
+  rc = encode_pages_map(c, k_pages, &map_k);
+  if (rc == LAVA_OK) rc = encode_pages_map(c, v_pages, &map_v);
+  if (rc != LAVA_OK) return rc;
+  const Portions portions = portions_of(c);
+  p.first_head = first_layer * c.batch * c.n_kv_heads;
+  p.heads = n_layers * c.batch * c.n_kv_heads;
+  p.subs = portions.subs;
+  p.per_sub = portions.per_sub;
   p.q = q;
-  p.k_pages = (const char*)k_pages;
-  p.v_pages = (const char*)v_pages;
   p.table = page_table;
   p.rows = head_rows;
   p.out = out;
   p.lse = lse;
-  const auto kernel = c.dtype == LAVA_BF16
-                          ? (c.head_dim == 64 ? decode_pages_kernel<64, true> : decode_pages_kernel<128, true>)
-                          : (c.head_dim == 64 ? decode_pages_kernel<64, false> : decode_pages_kernel<128, false>);
-  const cudaError_t e = launch_in_order(kernel, dim3(c.n_q_heads, n_layers * c.batch), kThreads, 0,
-                                        (cudaStream_t)stream, p);
-  count_launches(1);
-  return check_cuda(e, "paged decode attention launch");
+  char* ws = (char*)workspace;
+  p.status = (unsigned*)ws;
+  p.counters = (int*)(ws + kStatusBytes);
+  p.part = (float*)(ws + kStatusBytes + counter_bytes());
+  p.part_ml = (float2*)((char*)p.part + up256(slots_of(c) * c.head_dim * sizeof(float)));
+  p.wait_cycles = options().wait_limit_cycles;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (c.dtype == LAVA_BF16) {
+    if (c.head_dim == 128)
+      return portions.held == 8 ? launch<128, true, 8>(map_k, map_v, p, st) : launch<128, true, 16>(map_k, map_v, p, st);
+    return portions.held == 8 ? launch<64, true, 8>(map_k, map_v, p, st) : launch<64, true, 16>(map_k, map_v, p, st);
+  }
+  if (c.head_dim == 128)
+    return portions.held == 4 ? launch<128, false, 4>(map_k, map_v, p, st) : launch<128, false, 8>(map_k, map_v, p, st);
+  return portions.held == 4 ? launch<64, false, 4>(map_k, map_v, p, st) : launch<64, false, 8>(map_k, map_v, p, st);
 }
 
 }  // extern "C"

@@ -162,6 +162,9 @@ lava_status launch_score_sm100(const Geom& g, int n_layers, const void* q, const
 lava_status encode_score_maps(const Geom& g, int n_layers, const void* q, const void* k,
                               long long q_ls, long long k_ls, CUtensorMap* map_q,
                               CUtensorMap* map_k);
+// Tensor map of a paged cache's pool ([rows][d]) in boxes of 16 rows: blocks of 128 bytes of a row, with the
+// 128-byte swizzle, as a dimension of their own.
+lava_status encode_pages_map(const Cache& c, const void* pool, CUtensorMap* map);
 // Single-pass Blackwell score path (logits and exponentials stay in tensor memory).
 struct TmemLayout {
   int ok, nunit, tmax, kfold, gmax, heads_total, units_total;

@@ -1250,6 +1250,22 @@ static lava_status encode_query_map(const Geom& g, int n_layers, const void* q, 
   return LAVA_OK;
 }
 
+lava_status encode_pages_map(const Cache& c, const void* pool, CUtensorMap* map) {
+  EncodeTiledFn encode = encode_fn();
+  if (!encode) return fail(LAVA_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
+  const int es = c.dtype == LAVA_BF16 ? 2 : 4;
+  const cuuint64_t row_bytes = (cuuint64_t)c.head_dim * es, blocks = row_bytes / 128;
+  const cuuint64_t dims[3] = {(cuuint64_t)(128 / es), (cuuint64_t)c.n_pages << c.page_shift, blocks};
+  const cuuint64_t strides[2] = {row_bytes, 128};
+  const cuuint32_t box[3] = {(cuuint32_t)(128 / es), 16, (cuuint32_t)blocks}, step[3] = {1, 1, 1};
+  if (encode(map, es == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3,
+             const_cast<void*>(pool), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return fail(LAVA_ERR_CUDA, "tensor map of the pages could not be encoded");
+  return LAVA_OK;
+}
+
 // The maps of the single-pass kernel (head_dim 128): boxes of one block of 64 columns.
 lava_status encode_score_maps(const Geom& g, int n_layers, const void* q, const void* k,
                               long long q_ls, long long k_ls, CUtensorMap* map_q_out,
