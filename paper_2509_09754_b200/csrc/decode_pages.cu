@@ -48,6 +48,7 @@ struct Shape {
   static constexpr int kStages = 96 * 1024 / kStageBytes;
   static constexpr int kSmem = kStages * kStageBytes + 1024;     // (aligned to the swizzle's period inside)
   static_assert(kConsumers * Q * D * 4 <= kStageBytes, "the warps' results fit a stage");
+  static constexpr int kSmall = 128 * 1024 / kStageBytes, kLarge = 2 * kSmall;  // tiles of a piece
 };
 
 struct PageParams {
@@ -73,7 +74,21 @@ struct Ctl {
 };
 
 struct Start {
-  int head, sub, tile;  // head of the call, portion of its queries, tile
+  int head, sub, tile;     // head of the call, portion of its queries, tile
+  int end, first, pieces;  // a piece of a portion: its last tile + 1, the portion's first piece and their number
+};
+
+// Sums over heads (the host has seen to it that they fit).
+struct Counts {
+  int tiles, boxes, small, large;  // tiles, boxes of 16 rows, pieces of both sizes
+  int most;                        // boxes of the longest head
+  __device__ __forceinline__ void add(const Counts& y) {
+    tiles += y.tiles;
+    boxes += y.boxes;
+    small += y.small;
+    large += y.large;
+    most = max(most, y.most);
+  }
 };
 
 template <class S>
@@ -147,6 +162,7 @@ template <int D, int Q>
 struct TensorWarp {
   using S = Shape<D, true, Q>;
   static constexpr int kRowsOf = Q / 8;
+  static constexpr bool kOwnQueries = true;
   uint32_t qa[D / 16][2 * kRowsOf];
   float m[kRowsOf], l[kRowsOf], o[D / 8][4];
 
@@ -253,17 +269,35 @@ struct TensorWarp {
   }
   // column `col` of query q lies at float `col ^ swizzle(q)` of its row (spreads the rows over the banks)
   static __device__ __forceinline__ int swizzle(int q) { return (q & 7) * 8; }
-  __device__ __forceinline__ void leave_sums(float* to, const float2 (*stats)[Q]) {  // [Q][D] of this warp
+  // where in a stage warp i leaves column `col` of query q: in its own box of K, queries 8 to 15 in that of V
+  static __device__ __forceinline__ int sum_at(int i, int q, int col) {
+    return (q >> 3) * S::kTileBytes + i * S::kBoxBytes + ((q & 7) * D + (col ^ swizzle(q))) * 4;
+  }
+  static_assert(8 * D * 4 <= S::kBoxBytes, "eight queries' sums fit a box");
+  __device__ __forceinline__ float sum(int u, int nd, int e) const {  // column 8 nd + 2 t + e of query g + 8 u
+    return kRowsOf == 2 ? o[nd][2 * u + e] : o[nd][e] + o[nd][2 + e];
+  }
+  __device__ __forceinline__ void leave_sums(unsigned char* stage, int warp) {
+    const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+#pragma unroll
+    for (int u = 0; u < kRowsOf; ++u)
+#pragma unroll
+      for (int nd = 0; nd < D / 8; ++nd)
+        *reinterpret_cast<float2*>(stage + sum_at(warp, g + 8 * u, nd * 8 + 2 * t)) = make_float2(sum(u, nd, 0), sum(u, nd, 1));
+  }
+  // the output of a head that is this warp's alone
+  __device__ __forceinline__ void finish(const PageParams& p, size_t q_row, int queries) {
     const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
 #pragma unroll
     for (int u = 0; u < kRowsOf; ++u) {
-      const int q = g + 8 * u;
-      const float c = fast_exp2(m[u] - finite_ref(top_of<Q>(stats, q)));
+      l[u] += __shfl_xor_sync(0xffffffffu, l[u], 1);
+      l[u] += __shfl_xor_sync(0xffffffffu, l[u], 2);
+      if (g + 8 * u >= queries) continue;
+      const size_t row = q_row + g + 8 * u;
 #pragma unroll
-      for (int nd = 0; nd < D / 8; ++nd) {
-        const float a = kRowsOf == 2 ? o[nd][2 * u] : o[nd][0] + o[nd][2], b = kRowsOf == 2 ? o[nd][2 * u + 1] : o[nd][1] + o[nd][3];
-        *reinterpret_cast<float2*>(to + q * D + ((nd * 8 + 2 * t) ^ swizzle(q))) = make_float2(a * c, b * c);
-      }
+      for (int nd = 0; nd < D / 8; ++nd)
+        reinterpret_cast<uint32_t*>(p.out)[row * (D / 2) + nd * 4 + t] = pack_bf16(sum(u, nd, 0) / l[u], sum(u, nd, 1) / l[u]);
+      if (p.lse && t == 0) p.lse[row] = (m[u] + fast_log2(l[u])) * kLn2;
     }
   }
 };
@@ -275,15 +309,18 @@ template <int D, int Q>
 struct PlainWarp {
   using S = Shape<D, false, Q>;
   static constexpr int kRows = S::kWarpRows, kSplit = 32 / kRows, kPieces = D / 4 / kSplit, kCols = D / 32;
+  static constexpr bool kOwnQueries = kRows == kBoxRows;  // a copy per warp (which may have its own head), or one
   const float* qs;        // [Q][D] in shared memory
   float m[Q], l[Q], o[Q][kCols];
 
   __device__ __forceinline__ void begin(const PageParams& p, size_t q_row, int queries, float* q_mem) {
     // (all warps are through with the queries before: they have met)
-    for (int i = threadIdx.x; i < Q * (D / 4); i += kConsumers * 32)
+    if (kOwnQueries) __syncwarp();
+    for (int i = kOwnQueries ? threadIdx.x & 31 : threadIdx.x; i < Q * (D / 4); i += kOwnQueries ? 32 : kConsumers * 32)
       reinterpret_cast<float4*>(q_mem)[i] = i / (D / 4) < queries
           ? reinterpret_cast<const float4*>(p.q)[q_row * (D / 4) + i] : make_float4(0.f, 0.f, 0.f, 0.f);
-    meet();
+    if (kOwnQueries) __syncwarp();
+    else meet();
     qs = q_mem;
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
@@ -301,7 +338,7 @@ struct PlainWarp {
     float z[Q] = {};
 #pragma unroll 4
     for (int i = 0; i < kPieces; ++i) {
-      const int c = share * kPieces + i;
+      const int c = i * kSplit + share;  // (neighbouring pieces: no bank conflicts among the queries')
       float4 k;
       asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w)
                    : "r"(piece_at<S>(k_tile, r0 + row, c)));
@@ -346,10 +383,15 @@ struct PlainWarp {
         asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1])
                      : "r"(piece_at<S>(v_tile, r0 + r, lane / 2) + (lane & 1) * 8));
 #pragma unroll
-      for (int q = 0; q < Q; ++q) {
-        const float pr = probs[r * Q + q];
+      for (int q = 0; q < Q; q += 4) {
+        const float4 pr = *reinterpret_cast<const float4*>(probs + r * Q + q);
 #pragma unroll
-        for (int c = 0; c < kCols; ++c) o[q][c] = fmaf(pr, v[c], o[q][c]);
+        for (int c = 0; c < kCols; ++c) {
+          o[q][c] = fmaf(pr.x, v[c], o[q][c]);
+          o[q + 1][c] = fmaf(pr.y, v[c], o[q + 1][c]);
+          o[q + 2][c] = fmaf(pr.z, v[c], o[q + 2][c]);
+          o[q + 3][c] = fmaf(pr.w, v[c], o[q + 3][c]);
+        }
       }
     }
     return true;
@@ -363,14 +405,32 @@ struct PlainWarp {
       if ((threadIdx.x & 31) == 0) ml[q] = make_float2(m[q], l[q]);
     }
   }
-  static __device__ __forceinline__ int swizzle(int) { return 0; }
-  __device__ __forceinline__ void leave_sums(float* to, const float2 (*stats)[Q]) {
+  // where in a stage warp i leaves four columns from `col` on of query q: in its own box of K; or, where a box is two
+  // warps', in the q-th of its own rows
+  static __device__ __forceinline__ int sum_at(int i, int q, int col) {
+    return kRows == kBoxRows ? i * S::kBoxBytes + (q * D + col) * 4 : (int)piece_at<S>(0u, i * kRows + q, col / 4);
+  }
+  static_assert(Q * D * 4 <= kRows * S::kRowBytes, "the queries' sums fit a warp's rows");
+  __device__ __forceinline__ void leave_sums(unsigned char* stage, int warp) {
+    const int col = (threadIdx.x & 31) * kCols;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      float* to = reinterpret_cast<float*>(stage + sum_at(warp, q, col & ~3)) + (col & 3);
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) to[j] = o[q][j];
+    }
+  }
+  __device__ __forceinline__ void finish(const PageParams& p, size_t q_row, int queries) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-      const float c = fast_exp2(m[q] - finite_ref(top_of<Q>(stats, q)));
 #pragma unroll
-      for (int j = 0; j < kCols; ++j) to[q * D + lane * kCols + j] = o[q][j] * c;
+      for (int w = 16; w > 0; w >>= 1) l[q] += __shfl_xor_sync(0xffffffffu, l[q], w);
+      if (q >= queries) continue;
+      float* to = reinterpret_cast<float*>(p.out) + (q_row + q) * D + lane * kCols;
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) to[j] = o[q][j] / l[q];
+      if (p.lse && lane == 0) p.lse[q_row + q] = (m[q] + fast_log2(l[q])) * kLn2;
     }
   }
 };
@@ -430,19 +490,58 @@ __device__ __forceinline__ void join_parts(const PageParams& p, int w0, int n, i
   }
 }
 
+// How the line of tiles is cut (the same in every CTA: it follows from the row counts).
+struct Plan {
+  long long total;   // tiles of all portions
+  int parts;         // CTAs that have a part
+  int piece;         // > 0: a portion's tiles in pieces of at most so many, one per CTA; 0: equal parts of the line
+  int by_warp;       // 1: whole heads per warp
+};
+
+// Heads that are short against a warp's share go whole to warps, which then need not meet.  Else, where few CTAs have
+// work, a portion is cut into pieces of 128 or 256 KB, no more than there are CTAs; and where there is more, the line
+// into equal parts.
+template <class S>
+__device__ __forceinline__ Plan plan_of(const PageParams& p, const Counts& all) {
+  Plan plan = {(long long)all.tiles * p.subs, 0, 0, 0};
+  const long long grid = gridDim.x;
+  if (S::kWarpRows == kBoxRows && p.subs == 1 && 2 * all.most * grid * kConsumers <= all.boxes) {
+    plan.by_warp = 1;
+    plan.parts = (int)grid;
+  } else if ((long long)all.small * p.subs <= grid) {
+    plan.piece = S::kSmall;
+    plan.parts = all.small * p.subs;
+  } else if ((long long)all.large * p.subs <= grid) {
+    plan.piece = S::kLarge;
+    plan.parts = all.large * p.subs;
+  } else {
+    plan.parts = (int)min(grid, plan.total);
+  }
+  return plan;
+}
+
+// What a CTA leaves of a portion that others have parts of.
+struct Pending {
+  int w0, n, queries;  // parts w0 ... w0 + n - 1; n = 0: nothing
+  size_t q_row;
+};
+
 template <int D, bool BF16, int Q>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                     const __grid_constant__ PageParams p) {
   using S = Shape<D, BF16, Q>;
   using Warp = typename std::conditional<BF16, TensorWarp<D, Q>, PlainWarp<D, Q>>::type;
+  constexpr int kWarpsAll = kThreads / 32;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t full_k[S::kStages], full_v[S::kStages], empty[S::kStages];
   __shared__ Ctl ctl;
-  __shared__ int issued, last_one;
+  __shared__ int issued, last_one[2];
   __shared__ Start start;
+  __shared__ int cuts[kConsumers + 1], cut_at[kConsumers + 1];  // by warp: their first heads, and boxes before those
+  __shared__ Counts sums[kWarpsAll];
   __shared__ float2 stats[kConsumers][Q];
-  __shared__ __align__(16) float q_mem[BF16 ? 4 : Q * D];  // fp32: the queries
+  __shared__ __align__(16) float q_mem[BF16 ? 4 : (Warp::kOwnQueries ? kConsumers : 1) * Q * D];  // fp32: the queries
   __shared__ __align__(16) float prob_mem[BF16 ? 4 : kConsumers * S::kWarpRows * Q];
   const Cache& c = p.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -461,17 +560,18 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   }
   in_stream_order();
 
-  // ---- this CTA's part of the line of all tiles -----------------------------------------------------
-  long long total, at0, at1;
-  int parts;
+  // ---- the cut, and this CTA's part -----------------------------------------------------------------
+  Plan plan;
+  long long at0 = 0, at1 = 0;
   {
     const int share = (p.heads + kThreads - 1) / kThreads;
     const int h0 = min(p.heads, tid * share), h1 = min(p.heads, h0 + share);
-    int tiles = 0;
+    Counts mine = {};
 #pragma unroll 4
     for (int h = h0; h < h1; ++h) {
       const int len = head_len(p, h);
-      tiles += tiles_of<S>(len);
+      const int tiles = tiles_of<S>(len), boxes = (len + kBoxRows - 1) / kBoxRows;
+      mine.add({tiles, boxes, (tiles + S::kSmall - 1) / S::kSmall, (tiles + S::kLarge - 1) / S::kLarge, boxes});
       if (len == 0 && h % (int)gridDim.x == (int)blockIdx.x) {  // no rows: zeros
         const int prob = h / c.n_kv_heads, kvh = h - prob * c.n_kv_heads;
         const size_t row = (size_t)prob * c.n_q_heads + (size_t)kvh * c.group;
@@ -480,40 +580,66 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
           for (int i = 0; i < c.group; ++i) p.lse[row + i] = -INFINITY;
       }
     }
-    // (a head has 2^26 tiles at most, all heads of a pool without shared pages fewer; sums are kept in 64 bits)
-    long long incl = tiles;
+    const Counts of_warp = {__reduce_add_sync(0xffffffffu, mine.tiles), __reduce_add_sync(0xffffffffu, mine.boxes),
+                            __reduce_add_sync(0xffffffffu, mine.small), __reduce_add_sync(0xffffffffu, mine.large),
+                            __reduce_max_sync(0xffffffffu, mine.most)};
+    if (lane == 0) sums[warp] = of_warp;
+    __syncthreads();
+    Counts all = {}, warps_before = {};
+    for (int w = 0; w < kWarpsAll; ++w) {
+      if (w == warp) warps_before = all;
+      all.add(sums[w]);
+    }
+    plan = plan_of<S>(p, all);
+    if ((int)blockIdx.x >= plan.parts) return;
+    // what the cut counts, up to this thread's heads and in them
+    const auto counted = [&](const Counts& x) {
+      return plan.by_warp ? x.boxes : plan.piece == S::kSmall ? x.small : plan.piece ? x.large : x.tiles;
+    };
+    const int here = counted(mine);
+    int incl = here;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+      const int y = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += y;
     }
-    __shared__ long long sums[kThreads / 32];
-    if (lane == 31) sums[warp] = incl;
-    __syncthreads();
-    long long before = incl - tiles, all = 0;
-    for (int w = 0; w < kThreads / 32; ++w) {
-      if (w < warp) before += sums[w];
-      all += sums[w];
-    }
-    total = all * p.subs;
-    parts = (int)min((long long)gridDim.x, total);
-    if ((int)blockIdx.x >= parts) return;
-    at0 = total * blockIdx.x / parts;
-    at1 = total * (blockIdx.x + 1) / parts;
-    before *= p.subs;
-    if (at0 >= before && at0 < before + (long long)tiles * p.subs) {
-      int h = h0, n = tiles_of<S>(head_len(p, h));
-      long long at = before;
-      while (at + (long long)n * p.subs <= at0) {
-        at += (long long)n * p.subs;
-        n = tiles_of<S>(head_len(p, ++h));
+    const int before = counted(warps_before) + incl - here;
+    if (plan.by_warp) {
+      const long long workers = (long long)gridDim.x * kConsumers;
+      for (int k = 0; k <= kConsumers; ++k) {  // the first head whose boxes begin at the cut or behind it
+        const int cut = (int)(all.boxes * ((long long)blockIdx.x * kConsumers + k) / workers);
+        if (cut == 0 && tid == 0) cuts[k] = cut_at[k] = 0;
+        if (before < cut && cut <= before + here) {
+          int at = before, h = h0;
+          for (; at < cut; ++h) at += (head_len(p, h) + kBoxRows - 1) / kBoxRows;
+          cuts[k] = h;
+          cut_at[k] = at;
+        }
       }
-      start = {h, (int)((at0 - at) / n), (int)((at0 - at) % n)};
+    } else {
+      // the unit of the line, a tile or a piece, that this CTA's part begins with
+      at0 = plan.piece ? (long long)blockIdx.x : plan.total * blockIdx.x / plan.parts;
+      at1 = plan.total * (blockIdx.x + 1ll) / plan.parts;
+      const long long first = (long long)before * p.subs;
+      if (at0 >= first && at0 < first + (long long)here * p.subs) {
+        const int size = plan.piece ? plan.piece : 1;
+        const auto units = [&](int h) { return (tiles_of<S>(head_len(p, h)) + size - 1) / size; };
+        long long at = first;
+        int h = h0, n = units(h);
+        while (at + (long long)n * p.subs <= at0) {
+          at += (long long)n * p.subs;
+          n = units(++h);
+        }
+        const int sub = (int)((at0 - at) / n), i = (int)((at0 - at) % n);
+        const long long tiles = tiles_of<S>(head_len(p, h));
+        if (plan.piece)
+          start = {h, sub, (int)(tiles * i / n), (int)(tiles * (i + 1) / n), (int)at0 - i, n};
+        else
+          start = {h, sub, i, 0, 0, 0};
+      }
     }
     __syncthreads();
   }
-  long long left = at1 - at0;
-  int sub = start.sub, t0 = start.tile;  // of the head in hand; 0 in the heads that follow
   int stage = 0, use = 0;
   bool alive = true;
   const auto wait = [&](uint64_t* bar, int parity) {  // the same in all lanes
@@ -525,13 +651,92 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
       ++use;
     }
   };
+  // first row of the pool that a box of rows `row` ... is in (a page that is none of the pool: behind the pool's
+  // rows, where copies give zeros)
+  const auto place = [&](int h, int row) {
+    const int page = p.table[(size_t)(p.first_head + h) * c.max_pages + (row >> c.page_shift)];
+    return (unsigned)page < (unsigned)c.n_pages ? (page << c.page_shift) + (row & (c.page_rows - 1))
+                                                : c.n_pages << c.page_shift;
+  };
 
-  if (warp == kConsumers) {
+  if (plan.by_warp) {
+    if constexpr (S::kWarpRows == kBoxRows) {
+      int stages = 0;  // as many as the warp with most boxes has
+#pragma unroll
+      for (int k = 0; k < kConsumers; ++k) stages = max(stages, cut_at[k + 1] - cut_at[k]);
+      if (warp == kConsumers) {
+        // ---- producer: lanes 2 i and 2 i + 1 walk the heads of warp i, for K and for V; box i of a stage is warp i's
+        const int of = min(lane >> 1, kConsumers - 1);
+        const bool v = lane & 1, walks = lane < 2 * kConsumers;
+        int h = cuts[of], end = walks ? cuts[of + 1] : 0, row = 0, len = 0;
+        const auto advance = [&] {  // to the next row that begins a box, in a head that has rows
+          while (h < end && row >= len) {
+            if (len > 0) ++h;
+            len = h < end ? head_len(p, h) : 0;
+            row = 0;
+            if (len == 0 && h < end) ++h;
+          }
+        };
+        advance();
+        int at = h < end ? place(h, row) : 0;
+        for (; stages > 0; --stages) {
+          if (use > 0 && !(alive = wait(&empty[stage], (use - 1) & 1))) break;
+          const int boxes = __popc(__ballot_sync(0xffffffffu, h < end)) / 2;
+          if (lane == 0) {
+            mbar_expect_tx(smem_u32(&full_k[stage]), boxes * S::kBoxBytes);
+            mbar_expect_tx(smem_u32(&full_v[stage]), boxes * S::kBoxBytes);
+            ++issued;
+          }
+          __syncwarp();
+          if (h < end) {
+            tma_load_3d(ring + stage * S::kStageBytes + (v ? S::kTileBytes : 0) + of * S::kBoxBytes, v ? &map_v : &map_k, 0,
+                        at, 0, smem_u32(v ? &full_v[stage] : &full_k[stage]));
+            row += kBoxRows;
+            advance();
+            if (h < end) at = place(h, row);
+          }
+          next_stage();
+          __syncwarp();
+        }
+      } else {
+        // ---- consumers: their own heads
+        Warp w;
+        const Logit logit(c);
+        float* const probs = prob_mem + (BF16 ? 0 : warp * S::kWarpRows * Q);
+        for (int h = cuts[warp]; h < cuts[warp + 1] && alive; ++h) {
+          const int len = head_len(p, h);
+          if (len == 0) continue;
+          const int prob = h / c.n_kv_heads, kvh = h - prob * c.n_kv_heads;
+          const size_t q_row = (size_t)prob * c.n_q_heads + (size_t)kvh * c.group;
+          if constexpr (BF16) w.begin(p, q_row, c.group);
+          else w.begin(p, q_row, c.group, q_mem + warp * Q * D);
+          for (int row = 0; row < len; row += kBoxRows) {
+            const uint32_t k_tile = ring + stage * S::kStageBytes;
+            if (!(alive = wait(&full_k[stage], use & 1))) break;
+            alive = w.tile(k_tile, k_tile + S::kTileBytes, warp * kBoxRows, min(kBoxRows, len - row), logit, probs,
+                           [&] { return wait(&full_v[stage], use & 1); });
+            if (!alive) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
+            next_stage();
+            --stages;
+          }
+          if (alive) w.finish(p, q_row, c.group);
+        }
+        for (; stages > 0 && alive; --stages) {  // with boxes of other warps only
+          alive = wait(&full_k[stage], use & 1);
+          if (alive && lane == 0) mbar_arrive(smem_u32(&empty[stage]));
+          next_stage();
+        }
+      }
+    }
+  } else if (warp == kConsumers) {
     // ---- producer ----------------------------------------------------------------------------------
+    long long left = plan.piece ? start.end - start.tile : at1 - at0;
+    int sub = start.sub, t0 = start.tile;  // of the head in hand; 0 in the heads that follow
     for (int h = start.head; left > 0 && alive; ++h, sub = 0) {
       const int len = head_len(p, h), n = tiles_of<S>(len);
       if (n == 0) continue;
-      const int* pages = p.table + (size_t)(p.first_head + h) * c.max_pages;
       for (; sub < p.subs && left > 0 && alive; ++sub, t0 = 0) {
         const int t1 = (int)min((long long)n, t0 + left);
         left -= t1 - t0;
@@ -539,17 +744,8 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
           const int row0 = t * S::kTile;
           const int boxes = min(S::kTile / kBoxRows, (len - row0 + kBoxRows - 1) / kBoxRows);
           // lane 2 i + v: box i of K or V
-          const int row = row0 + (lane >> 1) * kBoxRows;
-          int at = 0;
-          if (lane < 2 * boxes) {
-            const int page = pages[row >> c.page_shift];
-            // (a page that is none of the pool: behind the pool's rows, where copies give zeros)
-            at = (unsigned)page < (unsigned)c.n_pages ? (page << c.page_shift) + (row & (c.page_rows - 1))
-                                                      : c.n_pages << c.page_shift;
-          }
-          if (use > 0) alive = wait(&empty[stage], (use - 1) & 1);
-          if (!alive) break;
-          const uint32_t k_tile = ring + stage * S::kStageBytes;
+          const int at = lane < 2 * boxes ? place(h, row0 + (lane >> 1) * kBoxRows) : 0;
+          if (use > 0 && !(alive = wait(&empty[stage], (use - 1) & 1))) break;
           if (lane == 0) {
             mbar_expect_tx(smem_u32(&full_k[stage]), boxes * S::kBoxBytes);
             mbar_expect_tx(smem_u32(&full_v[stage]), boxes * S::kBoxBytes);
@@ -558,8 +754,8 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
           __syncwarp();
           if (lane < 2 * boxes) {
             const bool v = lane & 1;
-            tma_load_3d(k_tile + (v ? S::kTileBytes : 0) + (lane >> 1) * S::kBoxBytes, v ? &map_v : &map_k, 0, at, 0,
-                        smem_u32(v ? &full_v[stage] : &full_k[stage]));
+            tma_load_3d(ring + stage * S::kStageBytes + (v ? S::kTileBytes : 0) + (lane >> 1) * S::kBoxBytes,
+                        v ? &map_v : &map_k, 0, at, 0, smem_u32(v ? &full_v[stage] : &full_k[stage]));
           }
           next_stage();
         }
@@ -570,6 +766,9 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     Warp w;
     const Logit logit(c);
     float* const probs = prob_mem + (BF16 ? 0 : warp * S::kWarpRows * Q);
+    Pending begun = {}, ended = {};  // the portion that the part begins in, and the one that it ends in
+    long long left = plan.piece ? start.end - start.tile : at1 - at0;
+    int sub = start.sub, t0 = start.tile;
     long long at = at0 - t0;  // first tile of the head's portion on the line
     for (int h = start.head; left > 0 && alive; ++h, sub = 0) {
       const int len = head_len(p, h), n = tiles_of<S>(len);
@@ -580,13 +779,13 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         const int queries = min(p.per_sub, c.group - sub * p.per_sub);
         const size_t q_row = (size_t)prob * c.n_q_heads + (size_t)kvh * c.group + sub * p.per_sub;
         if constexpr (BF16) w.begin(p, q_row, queries);
-        else w.begin(p, q_row, queries, q_mem);
+        else w.begin(p, q_row, queries, q_mem + (Warp::kOwnQueries ? warp * Q * D : 0));
         for (int t = t0; t < t1; ++t) {
           const uint32_t k_tile = ring + stage * S::kStageBytes, v_tile = k_tile + S::kTileBytes;
           const int r0 = warp * S::kWarpRows, valid = min(S::kWarpRows, len - t * S::kTile - r0);
-          alive = wait(&full_k[stage], use & 1);
+          if (!(alive = wait(&full_k[stage], use & 1))) break;
           const auto v_ready = [&] { return wait(&full_v[stage], use & 1); };
-          if (alive) alive = valid > 0 ? w.tile(k_tile, v_tile, r0, valid, logit, probs, v_ready) : v_ready();
+          alive = valid > 0 ? w.tile(k_tile, v_tile, r0, valid, logit, probs, v_ready) : v_ready();
           if (!alive) break;
           if (t + 1 < t1) {  // (the last stage is kept for the meeting)
             __syncwarp();
@@ -594,13 +793,14 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             next_stage();
           }
         }
-        // the warps meet: maxima and sums, then the sums of V against the common maximum
+        // The warps meet: each leaves its maxima and sums, and what it has summed of V in the memory of its own rows
+        // of the last stage, which no other warp reads.
+        unsigned char* const last = smem_raw + (ring - smem_u32(smem_raw)) + stage * S::kStageBytes;
         w.leave_stats(stats[warp]);
+        __syncwarp();
+        w.leave_sums(last, warp);
         alive = meet_all(alive);
         if (!alive) break;
-        float* const room = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)) + stage * S::kStageBytes);
-        w.leave_sums(room + warp * Q * D, stats);
-        meet();
         const bool whole = t0 == 0 && t1 == n;
         const size_t slot = (size_t)blockIdx.x * 2 + (t0 == 0);
         for (int e = tid; e < queries * (D / 4); e += kConsumers * 32) {
@@ -610,9 +810,10 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
           float l = 0.f;
 #pragma unroll
           for (int i = 0; i < kConsumers; ++i) {
-            const float4 f = *reinterpret_cast<const float4*>(room + (i * Q + q) * D + (col ^ Warp::swizzle(q)));
-            a = make_float4(a.x + f.x, a.y + f.y, a.z + f.z, a.w + f.w);
-            l = fmaf(stats[i][q].y, fast_exp2(stats[i][q].x - finite_ref(top)), l);
+            const float4 f = *reinterpret_cast<const float4*>(last + Warp::sum_at(i, q, col));
+            const float s = fast_exp2(stats[i][q].x - finite_ref(top));
+            a = make_float4(fmaf(f.x, s, a.x), fmaf(f.y, s, a.y), fmaf(f.z, s, a.z), fmaf(f.w, s, a.w));
+            l = fmaf(stats[i][q].y, s, l);
           }
           if (whole) {
             store4<BF16>(p.out, (q_row + q) * D + col, make_float4(a.x / l, a.y / l, a.z / l, a.w / l));
@@ -622,25 +823,39 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             if (col == 0) p.part_ml[slot * Q + q] = make_float2(top, l);
           }
         }
-        fence_async_proxy();  // (the room was written; the next copy into this stage comes after)
-        if (!whole) __threadfence();
+        fence_async_proxy();  // (the stage was written; the next copy into it comes after)
         meet();
         if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
         next_stage();
         if (!whole) {
-          // the parts that the portion's tiles `at` ... `at + n - 1` of the line lie in
-          const int w0 = (int)(((at + 1) * parts - 1) / total), w1 = (int)(((at + n) * parts - 1) / total);
-          if (tid == 0) last_one = atomicAdd(p.counters + w0, 1) == w1 - w0;
-          meet();
-          if (last_one) {
-            __threadfence();
-            join_parts<D, BF16, Q>(p, w0, w1 - w0 + 1, queries, q_row);
-            if (tid == 0) p.counters[w0] = 0;
+          // the parts that the portion's tiles lie in
+          Pending x = {start.first, start.pieces, queries, q_row};
+          if (!plan.piece) {
+            x.w0 = (int)(((at + 1) * plan.parts - 1) / plan.total);
+            x.n = (int)(((at + n) * plan.parts - 1) / plan.total) + 1 - x.w0;
           }
-          meet();  // (last_one is written again)
+          if (t0 == 0) ended = x;
+          else begun = x;
         }
         left -= t1 - t0;
         at += n;
+      }
+    }
+    // Portions that other CTAs have parts of, when this CTA is through: who comes last joins them.
+    if (alive && (begun.n || ended.n)) {
+      __threadfence();
+      meet();
+      if (tid == 0 && begun.n) last_one[0] = atomicAdd(p.counters + begun.w0, 1) == begun.n - 1;
+      if (tid == 32 && ended.n) last_one[1] = atomicAdd(p.counters + ended.w0, 1) == ended.n - 1;
+      meet();
+      __threadfence();
+      if (begun.n && last_one[0]) {
+        join_parts<D, BF16, Q>(p, begun.w0, begun.n, begun.queries, begun.q_row);
+        if (tid == 0) p.counters[begun.w0] = 0;
+      }
+      if (ended.n && last_one[1]) {
+        join_parts<D, BF16, Q>(p, ended.w0, ended.n, ended.queries, ended.q_row);
+        if (tid == 0) p.counters[ended.w0] = 0;
       }
     }
   }
@@ -713,6 +928,8 @@ lava_status lava_decode_attention_pages(const lava_cache_desc* cache, int32_t fi
     return fail(LAVA_ERR_INVALID_ARG, "NULL argument");
   if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out))
     return fail(LAVA_ERR_INVALID_ARG, "q, k_pages, v_pages and out must be 16-byte aligned");
+  if (((long long)n_layers * c.batch * c.n_kv_heads) >= (1ll << 35) / ((long long)c.max_pages << c.page_shift))
+    return fail(LAVA_ERR_UNSUPPORTED, "the heads of the call times the rows of a head must stay below 2^35");
   const size_t need = lava_cache_workspace_bytes(cache);
   if (!workspace || workspace_bytes < need)
     return fail(LAVA_ERR_WORKSPACE, "workspace too small: %zu < %zu bytes", workspace_bytes, need);
