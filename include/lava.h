@@ -509,7 +509,8 @@ LAVA_API lava_status lava_rotary_append(const lava_rotary_desc* rotary, const do
  *   lse         float [n_layers, batch, H_q], may be NULL
  *   page_table, head_rows   of the whole cache
  *   workspace   lava_cache_workspace_bytes(cache) bytes, zeroed once
- * The heads of a call times max_pages * page_rows stay below 2^35.  A head without rows gives zeros and lse = -infinity.  Sums, maxima and the output before its last
+ * The heads of a call times max_pages * page_rows stay below 2^35 (times the portions of 16 queries, 8 with
+ * fp32, that a group has).  A head without rows gives zeros and lse = -infinity.  Sums, maxima and the output before its last
  * rounding are fp32; with bf16 the probabilities enter the product with V as two bf16 terms (relative
  * error below 2^-16).  The split of the rows over blocks depends on all row counts of the call, so the
  * last bits may too; the same call gives the same bits. */

@@ -54,16 +54,17 @@ struct Shape {
 struct PageParams {
   Cache c;
   int first_head;          // of the call's first layer
-  int heads;               // of the call's layers
+  int heads, queries;      // of the call's layers
   int subs, per_sub;       // a group's queries are taken in `subs` portions of `per_sub`
+  int own_queries;         // a warp can have a head of its own
   const void* q;           // [layers, batch, H_q, d]
   const int* table;
   const int* rows;
   void* out;
   float* lse;
-  float* part;             // [CTA][2][Q][D]: partial results of the part's first and last head,
+  float* part;             // [CTA][2][Q][D]: partial results of the part's first and last portion,
   float2* part_ml;         // [CTA][2][Q]: the maximum that they are relative to, and the sum
-  int* counters;           // [CTA]: parts that have left their result of the head that begins last in CTA's part
+  int* counters;           // [CTA]: CTAs that have left their result of the portion that begins last in this one's part
   unsigned* status;
   long long wait_cycles;
 };
@@ -73,28 +74,33 @@ struct Ctl {
   long long wait_cycles;
 };
 
-struct Start {
-  int head, sub, tile;     // head of the call, portion of its queries, tile
-  int end, first, pieces;  // a piece of a portion: its last tile + 1, the portion's first piece and their number
-};
-
+template <class S>
+__device__ __forceinline__ int tiles_of(int len) {
+  return (len + S::kTile - 1) / S::kTile;
+}
 // Sums over heads (the host has seen to it that they fit).
 struct Counts {
   int tiles, boxes, small, large;  // tiles, boxes of 16 rows, pieces of both sizes
-  int most;                        // boxes of the longest head
+  int most, empty;                 // boxes of the longest head; heads without rows
+  template <class S>
+  static __device__ __forceinline__ Counts of(int len) {
+    const int tiles = tiles_of<S>(len), boxes = (len + kBoxRows - 1) / kBoxRows;
+    return {tiles, boxes, (tiles + S::kSmall - 1) / S::kSmall, (tiles + S::kLarge - 1) / S::kLarge, boxes, len == 0};
+  }
   __device__ __forceinline__ void add(const Counts& y) {
     tiles += y.tiles;
     boxes += y.boxes;
     small += y.small;
     large += y.large;
     most = max(most, y.most);
+    empty += y.empty;
+  }
+  __device__ __forceinline__ Counts over_warp() const {
+    return {__reduce_add_sync(0xffffffffu, tiles), __reduce_add_sync(0xffffffffu, boxes),
+            __reduce_add_sync(0xffffffffu, small), __reduce_add_sync(0xffffffffu, large),
+            __reduce_max_sync(0xffffffffu, most), __reduce_add_sync(0xffffffffu, empty)};
   }
 };
-
-template <class S>
-__device__ __forceinline__ int tiles_of(int len) {
-  return (len + S::kTile - 1) / S::kTile;
-}
 __device__ __forceinline__ int head_len(const PageParams& p, int h) {
   return min(max(0, p.rows[p.first_head + h]), p.c.max_pages << p.c.page_shift);
 }
@@ -162,21 +168,39 @@ template <int D, int Q>
 struct TensorWarp {
   using S = Shape<D, true, Q>;
   static constexpr int kRowsOf = Q / 8;
-  static constexpr bool kOwnQueries = true;
-  uint32_t qa[D / 16][2 * kRowsOf];
+  // The queries lie in shared memory as the A operand's fragments, 16 bytes per lane: a copy per warp, which may have a
+  // head of its own, or one (16 queries of 128 leave no room for four).  The next head's are on their way in registers.
+  static constexpr int kFrags = D / 16 * 2 * kRowsOf / 4;
+  static constexpr bool kOwnQueries = Q * D <= 1024;
+  static constexpr int kNext = kOwnQueries ? kFrags : kFrags / kConsumers;
+  static constexpr int kQueryBytes = kFrags * 512;  // of a copy
+  uint4 next[kNext];
   float m[kRowsOf], l[kRowsOf], o[D / 8][4];
 
-  __device__ __forceinline__ void begin(const PageParams& p, size_t q_row, int queries) {
-    const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+  __device__ __forceinline__ void fetch(const PageParams& p, size_t q_row, int queries) {
+    const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3, first = kOwnQueries ? 0 : (threadIdx.x >> 5) * kNext;
+    const uint32_t* qh = reinterpret_cast<const uint32_t*>(p.q) + (q_row + g) * (D / 2) + t;
+#pragma unroll
+    for (int j = 0; j < kNext; ++j) {
+      const int i = first + j;  // k-steps 2 i and 2 i + 1 of rows g, or k-step i of rows g and g + 8
+      const uint32_t* lo = qh + (kRowsOf == 1 ? 16 : 8) * i;
+      const uint32_t* hi = kRowsOf == 1 ? lo + 8 : lo + 8 * (D / 2);
+      const bool there = g < queries, other = kRowsOf == 1 ? there : g + 8 < queries;
+      next[j] = kRowsOf == 1 ? make_uint4(there ? lo[0] : 0u, there ? lo[4] : 0u, there ? hi[0] : 0u, there ? hi[4] : 0u)
+                             : make_uint4(there ? lo[0] : 0u, other ? hi[0] : 0u, there ? lo[4] : 0u, other ? hi[4] : 0u);
+    }
+  }
+
+  // a head begins, whose queries have been fetched
+  __device__ __forceinline__ void begin(unsigned char* q_mem) {
+    const int lane = threadIdx.x & 31, first = kOwnQueries ? 0 : (threadIdx.x >> 5) * kNext;
+    __syncwarp();  // (in a shared copy: all warps are through with the queries before, they have met)
+#pragma unroll
+    for (int j = 0; j < kNext; ++j) reinterpret_cast<uint4*>(q_mem)[(first + j) * 32 + lane] = next[j];
+    if (kOwnQueries) __syncwarp();
+    else meet();
 #pragma unroll
     for (int u = 0; u < kRowsOf; ++u) {
-      const bool there = g + 8 * u < queries;
-      const uint32_t* qh = reinterpret_cast<const uint32_t*>(p.q) + (q_row + g + 8 * u) * (D / 2);
-#pragma unroll
-      for (int s = 0; s < D / 16; ++s) {
-        qa[s][u] = there ? qh[8 * s + t] : 0u;
-        qa[s][kRowsOf + u] = there ? qh[8 * s + 4 + t] : 0u;
-      }
       m[u] = -INFINITY;
       l[u] = 0.f;
     }
@@ -184,20 +208,23 @@ struct TensorWarp {
     for (int nd = 0; nd < D / 8; ++nd) o[nd][0] = o[nd][1] = o[nd][2] = o[nd][3] = 0.f;
   }
 
-  // rows r0 ... r0 + 15 of the tile, of which `valid` (> 0) are there; v_ready() waits for V
-  template <class Wait>
-  __device__ __forceinline__ bool tile(uint32_t k_tile, uint32_t v_tile, int r0, int valid, const Logit& logit, float*,
-                                       Wait v_ready) {
+  // rows r0 ... r0 + 15 of the tile, of which `valid` (> 0) are there
+  __device__ __forceinline__ void tile(uint32_t k_tile, uint32_t v_tile, int r0, int valid, const Logit& logit,
+                                       const unsigned char* q_mem, float*) {
     const int lane = threadIdx.x & 31, t = lane & 3, mi = lane >> 3, r8 = lane & 7;
-    float s[2][4] = {};
+    float s[2][4] = {}, s2[2][4] = {};  // odd k-steps have sums of their own: shorter chains
+    uint4 qa = {};
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {  // matrices (keys 0-7, piece 2 ks), (0-7, 2 ks + 1), (8-15, ...)
       uint32_t b0, b1, b2, b3;
       ldmatrix_x4(b0, b1, b2, b3, piece_at<S>(k_tile, r0 + (mi >> 1) * 8 + r8, 2 * ks + (mi & 1)));
-      const uint32_t a0 = qa[ks][0], a1 = kRowsOf == 2 ? qa[ks][1] : 0u;
-      const uint32_t a2 = qa[ks][kRowsOf], a3 = kRowsOf == 2 ? qa[ks][kRowsOf + 1] : 0u;
-      mma_bf16_16816(s[0][0], s[0][1], s[0][2], s[0][3], a0, a1, a2, a3, b0, b1);
-      mma_bf16_16816(s[1][0], s[1][1], s[1][2], s[1][3], a0, a1, a2, a3, b2, b3);
+      if (kRowsOf == 2 || ks % 2 == 0)
+        qa = reinterpret_cast<const uint4*>(q_mem)[(kRowsOf == 2 ? ks : ks / 2) * 32 + lane];
+      const uint32_t a0 = kRowsOf == 2 || ks % 2 == 0 ? qa.x : qa.z, a1 = kRowsOf == 2 ? qa.y : 0u;
+      const uint32_t a2 = kRowsOf == 2 ? qa.z : ks % 2 == 0 ? qa.y : qa.w, a3 = kRowsOf == 2 ? qa.w : 0u;
+      float (&to)[2][4] = ks % 2 ? s2 : s;
+      mma_bf16_16816(to[0][0], to[0][1], to[0][2], to[0][3], a0, a1, a2, a3, b0, b1);
+      mma_bf16_16816(to[1][0], to[1][1], to[1][2], to[1][3], a0, a1, a2, a3, b2, b3);
     }
     uint32_t hi[2][kRowsOf], lo[2][kRowsOf];  // [keys 0-7, 8-15][row]
     float corr[kRowsOf];
@@ -209,7 +236,7 @@ struct TensorWarp {
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          x[n][e] = 8 * n + 2 * t + e < valid ? logit.of(s[n][2 * u + e]) : -INFINITY;
+          x[n][e] = 8 * n + 2 * t + e < valid ? logit.of(s[n][2 * u + e] + s2[n][2 * u + e]) : -INFINITY;
           best = fmaxf(best, x[n][e]);
         }
       best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
@@ -233,7 +260,6 @@ struct TensorWarp {
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[nd][e] *= corr[kRowsOf == 2 ? e >> 1 : 0];
     }
-    if (!v_ready()) return false;
     if (valid < 16) {  // rows behind the last one may hold anything: their probabilities are 0, so must they be
       for (int i = lane; i < (16 - valid) * (D / 8); i += 32)
         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(piece_at<S>(v_tile, r0 + valid + i / (D / 8), i % (D / 8))),
@@ -255,7 +281,6 @@ struct TensorWarp {
         mma_bf16_16816(o[nd + 1][0], o[nd + 1][1], o[nd + 1][2], o[nd + 1][3], hi[0][0], hi[0][1], hi[1][0], hi[1][1], b2, b3);
       }
     }
-    return true;
   }
 
   __device__ __forceinline__ void leave_stats(float2* ml) {  // [Q] of this warp
@@ -294,9 +319,10 @@ struct TensorWarp {
       l[u] += __shfl_xor_sync(0xffffffffu, l[u], 2);
       if (g + 8 * u >= queries) continue;
       const size_t row = q_row + g + 8 * u;
+      const float inv = 1.f / l[u];
 #pragma unroll
       for (int nd = 0; nd < D / 8; ++nd)
-        reinterpret_cast<uint32_t*>(p.out)[row * (D / 2) + nd * 4 + t] = pack_bf16(sum(u, nd, 0) / l[u], sum(u, nd, 1) / l[u]);
+        reinterpret_cast<uint32_t*>(p.out)[row * (D / 2) + nd * 4 + t] = pack_bf16(sum(u, nd, 0) * inv, sum(u, nd, 1) * inv);
       if (p.lse && t == 0) p.lse[row] = (m[u] + fast_log2(l[u])) * kLn2;
     }
   }
@@ -310,18 +336,29 @@ struct PlainWarp {
   using S = Shape<D, false, Q>;
   static constexpr int kRows = S::kWarpRows, kSplit = 32 / kRows, kPieces = D / 4 / kSplit, kCols = D / 32;
   static constexpr bool kOwnQueries = kRows == kBoxRows;  // a copy per warp (which may have its own head), or one
-  const float* qs;        // [Q][D] in shared memory
+  static constexpr int kQueryBytes = Q * D * 4;
+  static constexpr int kNext = Q * D / 4 / (kOwnQueries ? 32 : 32 * kConsumers);
+  static_assert(kNext >= 1, "a lane has a piece of the queries");
+  uint4 next[kNext];      // of the queries of the next head
   float m[Q], l[Q], o[Q][kCols];
 
-  __device__ __forceinline__ void begin(const PageParams& p, size_t q_row, int queries, float* q_mem) {
-    // (all warps are through with the queries before: they have met)
-    if (kOwnQueries) __syncwarp();
-    for (int i = kOwnQueries ? threadIdx.x & 31 : threadIdx.x; i < Q * (D / 4); i += kOwnQueries ? 32 : kConsumers * 32)
-      reinterpret_cast<float4*>(q_mem)[i] = i / (D / 4) < queries
-          ? reinterpret_cast<const float4*>(p.q)[q_row * (D / 4) + i] : make_float4(0.f, 0.f, 0.f, 0.f);
+  __device__ __forceinline__ void fetch(const PageParams& p, size_t q_row, int queries) {
+    const int first = kOwnQueries ? threadIdx.x & 31 : threadIdx.x;
+#pragma unroll
+    for (int j = 0; j < kNext; ++j) {
+      const int i = first + j * (kOwnQueries ? 32 : 32 * kConsumers);
+      next[j] = i / (D / 4) < queries ? reinterpret_cast<const uint4*>(p.q)[q_row * (D / 4) + i] : uint4{};
+    }
+  }
+
+  __device__ __forceinline__ void begin(unsigned char* q_mem) {
+    const int first = kOwnQueries ? threadIdx.x & 31 : threadIdx.x;
+    __syncwarp();  // (in a shared copy: all warps are through with the queries before, they have met)
+#pragma unroll
+    for (int j = 0; j < kNext; ++j)
+      reinterpret_cast<uint4*>(q_mem)[first + j * (kOwnQueries ? 32 : 32 * kConsumers)] = next[j];
     if (kOwnQueries) __syncwarp();
     else meet();
-    qs = q_mem;
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
       m[q] = -INFINITY;
@@ -331,10 +368,10 @@ struct PlainWarp {
     }
   }
 
-  template <class Wait>
-  __device__ __forceinline__ bool tile(uint32_t k_tile, uint32_t v_tile, int r0, int valid, const Logit& logit,
-                                       float* probs, Wait v_ready) {
+  __device__ __forceinline__ void tile(uint32_t k_tile, uint32_t v_tile, int r0, int valid, const Logit& logit,
+                                       const unsigned char* q_mem, float* probs) {
     const int lane = threadIdx.x & 31, row = lane % kRows, share = lane / kRows;
+    const float* qs = reinterpret_cast<const float*>(q_mem);  // [Q][D]
     float z[Q] = {};
 #pragma unroll 4
     for (int i = 0; i < kPieces; ++i) {
@@ -371,7 +408,6 @@ struct PlainWarp {
       for (int q = 0; q < Q; q += 4)
         *reinterpret_cast<float4*>(probs + row * Q + q) = make_float4(z[q], z[q + 1], z[q + 2], z[q + 3]);
     __syncwarp();
-    if (!v_ready()) return false;
 #pragma unroll 4
     for (int r = 0; r < kRows; ++r) {
       if (r >= valid) break;  // rows behind the last one may hold anything
@@ -394,7 +430,6 @@ struct PlainWarp {
         }
       }
     }
-    return true;
   }
 
   __device__ __forceinline__ void leave_stats(float2* ml) {
@@ -443,59 +478,12 @@ __device__ __forceinline__ void store4(void* out, size_t at, float4 x) {  // `at
     *reinterpret_cast<float4*>(reinterpret_cast<float*>(out) + at) = x;
 }
 
-// The partial results of `n` parts of a head, from CTA `w0` on (there the last of its part, then the first ones),
-// joined in order: a warp per query.
-template <int D, bool BF16, int Q>
-__device__ __forceinline__ void join_parts(const PageParams& p, int w0, int n, int queries, size_t q_row) {
-  constexpr int kCols = D / 32, kAhead = 8;
-  using Cols = typename std::conditional<D == 128, float4, float2>::type;
-  const int lane = threadIdx.x & 31;
-  auto slot = [&](int i) { return (size_t)(w0 + i) * 2 + (i == 0); };
-  for (int q = threadIdx.x >> 5; q < queries; q += kConsumers) {
-    float top = -INFINITY;
-    for (int i = lane; i < n; i += 32) top = fmaxf(top, __ldcg(p.part_ml + slot(i) * Q + q).x);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float ref = finite_ref(top);
-    float acc[kCols] = {}, l = 0.f;
-    for (int s0 = 0; s0 < n; s0 += 32) {
-      const float2 ml = s0 + lane < n ? __ldcg(p.part_ml + slot(s0 + lane) * Q + q) : make_float2(-INFINITY, 0.f);
-      const float w = fast_exp2(ml.x - ref);
-      const int end = min(32, n - s0);
-      for (int i0 = 0; i0 < end; i0 += kAhead) {
-        Cols v[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-          if (i0 + j < end) v[j] = __ldcg(reinterpret_cast<const Cols*>(p.part + (slot(s0 + i0 + j) * Q + q) * D) + lane);
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-          if (i0 + j >= end) break;
-          const float wi = __shfl_sync(0xffffffffu, w, i0 + j);
-          const float* f = reinterpret_cast<const float*>(&v[j]);
-#pragma unroll
-          for (int c = 0; c < kCols; ++c) acc[c] = fmaf(wi, f[c], acc[c]);
-          l = fmaf(wi, __shfl_sync(0xffffffffu, ml.y, i0 + j), l);
-        }
-      }
-    }
-    const size_t at = (q_row + q) * D + lane * kCols;
-    if constexpr (D == 128) {
-      store4<BF16>(p.out, at, make_float4(acc[0] / l, acc[1] / l, acc[2] / l, acc[3] / l));
-    } else if constexpr (BF16) {
-      *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.out) + at) = pack_bf16(acc[0] / l, acc[1] / l);
-    } else {
-      *reinterpret_cast<float2*>(reinterpret_cast<float*>(p.out) + at) = make_float2(acc[0] / l, acc[1] / l);
-    }
-    if (p.lse && lane == 0) p.lse[q_row + q] = (top + fast_log2(l)) * kLn2;
-  }
-}
-
 // How the line of tiles is cut (the same in every CTA: it follows from the row counts).
 struct Plan {
-  long long total;   // tiles of all portions
-  int parts;         // CTAs that have a part
-  int piece;         // > 0: a portion's tiles in pieces of at most so many, one per CTA; 0: equal parts of the line
-  int by_warp;       // 1: whole heads per warp
+  int by_warp;  // 1: whole heads per warp
+  int piece;    // > 0: a portion's tiles in pieces of at most so many, one per CTA
+  int parts;    // CTAs that have a part
+  int total;    // tiles of all portions (the host has seen to it that 32 bits hold them)
 };
 
 // Heads that are short against a warp's share go whole to warps, which then need not meet.  Else, where few CTAs have
@@ -503,317 +491,516 @@ struct Plan {
 // into equal parts.
 template <class S>
 __device__ __forceinline__ Plan plan_of(const PageParams& p, const Counts& all) {
-  Plan plan = {(long long)all.tiles * p.subs, 0, 0, 0};
-  const long long grid = gridDim.x;
-  if (S::kWarpRows == kBoxRows && p.subs == 1 && 2 * all.most * grid * kConsumers <= all.boxes) {
+  Plan plan = {0, 0, 0, all.tiles * p.subs};
+  const int grid = gridDim.x;
+  if (S::kWarpRows == kBoxRows && p.subs == 1 && p.own_queries && (long long)all.most * grid * kConsumers <= 2ll * all.boxes) {
     plan.by_warp = 1;
-    plan.parts = (int)grid;
-  } else if ((long long)all.small * p.subs <= grid) {
+    plan.parts = grid;
+  } else if (all.small * p.subs <= grid) {
     plan.piece = S::kSmall;
     plan.parts = all.small * p.subs;
-  } else if ((long long)all.large * p.subs <= grid) {
+  } else if (all.large * p.subs <= grid) {
     plan.piece = S::kLarge;
     plan.parts = all.large * p.subs;
   } else {
-    plan.parts = (int)min(grid, plan.total);
+    plan.parts = min(grid, plan.total);
   }
   return plan;
 }
+// The line of `total` units in `parts` parts of equal size, the first total % parts of them one longer: where part i
+// begins, and the part that unit u is in.
+__device__ __forceinline__ int part_begin(int total, int parts, int i) {
+  return total / parts * i + min(i, total % parts);
+}
+__device__ __forceinline__ int part_of(int total, int parts, int u) {
+  const int size = total / parts, longer = total % parts;
+  return u < longer * (size + 1) ? u / (size + 1) : longer + (u - longer * (size + 1)) / size;
+}
 
-// What a CTA leaves of a portion that others have parts of.
+// A CTA's part: its first tile, and how many it has.
+struct Part {
+  int head, sub, tile;   // head of the call, portion of its queries, tile in it
+  int tiles;
+  int first, pieces;     // of a piece: the portion's first piece and their number
+};
+
+// A portion that other CTAs have tiles of too: those from CTA w0 on, n of them (0: there is none).
 struct Pending {
-  int w0, n, queries;  // parts w0 ... w0 + n - 1; n = 0: nothing
+  int w0, n, queries;
   size_t q_row;
 };
+
+template <int D, bool BF16, int Q>
+using WarpOf = typename std::conditional<BF16, TensorWarp<D, Q>, PlainWarp<D, Q>>::type;
+
+constexpr int kSegs = 64;  // segments of heads that are counted, at most
+
+template <int D, bool BF16, int Q>
+struct Shared {
+  using S = Shape<D, BF16, Q>;
+  using Warp = WarpOf<D, BF16, Q>;
+  uint64_t full[S::kStages], empty[S::kStages];
+  uint64_t full_own[S::kStages][kConsumers];           // by warp: of its box of a stage
+  Ctl ctl;
+  int issued, last_one[2];
+  Pending pending[2];                                  // the portions that the part begins and ends in
+  Counts segs[kSegs];
+  float2 stats[kConsumers][Q];
+  alignas(16) unsigned char q_mem[Warp::kOwnQueries ? kConsumers : 1][Warp::kQueryBytes];
+  alignas(16) float probs[BF16 ? 1 : kConsumers][BF16 ? 4 : S::kWarpRows * Q];
+};
+
+// First row of the pool that the box of rows `row` ... of a head is in (a page that is none of the pool: behind the
+// pool's rows, where copies give zeros).
+__device__ __forceinline__ int place(const PageParams& p, int h, int row) {
+  const Cache& c = p.c;
+  const int page = p.table[(size_t)(p.first_head + h) * c.max_pages + (row >> c.page_shift)];
+  return (unsigned)page < (unsigned)c.n_pages ? (page << c.page_shift) + (row & (c.page_rows - 1))
+                                              : c.n_pages << c.page_shift;
+}
+// First row of the outputs, and of the queries, of a head's first query.
+__device__ __forceinline__ size_t first_query(const Cache& c, int h) {
+  const int prob = h / c.n_kv_heads, kvh = h - prob * c.n_kv_heads;
+  return (size_t)prob * c.n_q_heads + (size_t)kvh * c.group;
+}
+// Inclusive prefix sum over the warp.
+__device__ __forceinline__ int scan_warp(int x) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+// The head that unit u of all heads' units is in, and how many units lie before that head; counted(x) picks the units
+// of a head or a segment.  For whole warps.
+template <class S, class Counted>
+__device__ __forceinline__ int2 find_unit(const PageParams& p, const Counts* segs, int seg_heads, int u, Counted counted) {
+  const int lane = threadIdx.x & 31;
+  int at = 0, seg = 0;
+  for (;; seg += 32) {
+    const int mine = (seg + lane) * seg_heads < p.heads ? counted(segs[seg + lane]) : 0;
+    const int upto = scan_warp(mine);
+    const unsigned past = __ballot_sync(0xffffffffu, at + upto > u);
+    if (past) {
+      const int i = __ffs(past) - 1;
+      at += __shfl_sync(0xffffffffu, upto - mine, i);
+      seg += i;
+      break;
+    }
+    at += __shfl_sync(0xffffffffu, upto, 31);
+    if ((seg + 32) * seg_heads >= p.heads) return make_int2(p.heads, at);  // behind the last unit
+  }
+  for (int h = seg * seg_heads;; h += 32) {
+    const int mine = h + lane < p.heads ? counted(Counts::of<S>(head_len(p, h + lane))) : 0;
+    const int upto = scan_warp(mine);
+    const unsigned past = __ballot_sync(0xffffffffu, at + upto > u);
+    if (past) {
+      const int i = __ffs(past) - 1;
+      return make_int2(h + i, at + __shfl_sync(0xffffffffu, upto - mine, i));
+    }
+    at += __shfl_sync(0xffffffffu, upto, 31);
+  }
+}
+
+// One warp's heads [h, end) of `boxes` boxes in all, alone: it fetches its own boxes, a place in every stage.  32 boxes
+// at a time are looked up, a lane each, and the next 32 while these are worked on.
+template <int D, bool BF16, int Q>
+__device__ __forceinline__ void whole_heads(const PageParams& p, const CUtensorMap* map_k, const CUtensorMap* map_v,
+                                            Shared<D, BF16, Q>& sh, uint32_t ring, int h, int end, int boxes) {
+  using S = Shape<D, BF16, Q>;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  unsigned char* const q_mem = sh.q_mem[WarpOf<D, BF16, Q>::kOwnQueries ? warp : 0];
+  WarpOf<D, BF16, Q> w;
+  const Logit logit(p.c);
+  struct Batch {
+    int head, row, len, at, q_row;  // this lane's box
+  };
+  int next_head = h, next_row = 0;  // the first box that is not in a batch yet
+  const auto look_up = [&] {
+    Batch b = {end, 0, 0, 0, 0};
+    int n = 0;  // boxes in the batch
+    while (n < 32 && next_head < end) {
+      // boxes of the next 32 heads, counted on from those in hand
+      const int len = next_head + lane < end ? head_len(p, next_head + lane) : 0;
+      const int upto = scan_warp((len + kBoxRows - 1) / kBoxRows - (lane == 0 ? next_row / kBoxRows : 0));
+      const int want = lane - n;    // which of these boxes is this lane's
+      int of = 0;                   // the head that it is in: as many heads end before it or with it
+#pragma unroll
+      for (int step = 16; step > 0; step >>= 1)
+        if (__shfl_sync(0xffffffffu, upto, of + step - 1) <= want) of += step;
+      const int all = __shfl_sync(0xffffffffu, upto, 31);
+      const int ended = __shfl_sync(0xffffffffu, upto, max(0, of - 1)), before = of > 0 ? ended : 0;
+      const int its_len = __shfl_sync(0xffffffffu, len, of);
+      if (want >= 0 && want < all) {
+        b.head = next_head + of;
+        b.row = (want - before) * kBoxRows + (of == 0 ? next_row : 0);
+        b.len = its_len;
+      }
+      const int took = min(32 - n, all);
+      if (took < all) {  // the batch is full inside these heads
+        const int lh = __shfl_sync(0xffffffffu, b.head, 31), lr = __shfl_sync(0xffffffffu, b.row, 31);
+        const int ll = __shfl_sync(0xffffffffu, b.len, 31);
+        next_head = lr + kBoxRows < ll ? lh : lh + 1;
+        next_row = lr + kBoxRows < ll ? lr + kBoxRows : 0;
+      } else {
+        next_head = min(end, next_head + 32);
+        next_row = 0;
+      }
+      n += took;
+    }
+    if (lane < n) {
+      b.at = place(p, b.head, b.row);
+      b.q_row = (int)first_query(p.c, b.head);
+    }
+    return b;
+  };
+  Batch cur = look_up(), nxt = look_up();
+  int sent = 0, first = 0;  // boxes asked for; number of the first of `cur`
+  const auto send = [&] {
+    const int i = sent - first;
+    const int at = __shfl_sync(0xffffffffu, i < 32 ? cur.at : nxt.at, i & 31), stage = sent % S::kStages;
+    const uint32_t bar = smem_u32(&sh.full_own[stage][warp]);
+    if (lane == 0) mbar_expect_tx(bar, 2 * S::kBoxBytes);
+    __syncwarp();
+    if (lane < 2)
+      tma_load_3d(ring + stage * S::kStageBytes + lane * S::kTileBytes + warp * S::kBoxBytes, lane ? map_v : map_k, 0, at, 0, bar);
+    ++sent;
+  };
+  while (sent < min(boxes, S::kStages)) send();
+  int in_hand = -1, fetched = -1;
+  bool alive = true;
+  for (int i = 0; i < boxes; ++i) {
+    if (i - first == 32) {
+      cur = nxt;
+      first += 32;
+      nxt = look_up();
+    }
+    const int head = __shfl_sync(0xffffffffu, cur.head, i - first), row = __shfl_sync(0xffffffffu, cur.row, i - first);
+    const int len = __shfl_sync(0xffffffffu, cur.len, i - first), stage = i % S::kStages;
+    const int q_row = __shfl_sync(0xffffffffu, cur.q_row, i - first);
+    if (head != in_hand) {
+      if (fetched != q_row) w.fetch(p, q_row, p.c.group);
+      w.begin(q_mem);
+      in_hand = head;
+      // the next head's, in case it follows (queries of neighbouring heads are neighbours)
+      fetched = min(q_row + p.c.group, p.queries - p.c.group);
+      w.fetch(p, fetched, p.c.group);
+    }
+    alive = __all_sync(0xffffffffu, wait_bar(smem_u32(&sh.full_own[stage][warp]), (i / S::kStages) & 1, &sh.ctl, p.status));
+    if (!alive) break;
+    const uint32_t k_tile = ring + stage * S::kStageBytes;
+    w.tile(k_tile, k_tile + S::kTileBytes, warp * kBoxRows, min(kBoxRows, len - row), logit, q_mem,
+           sh.probs[BF16 ? 0 : warp]);
+    __syncwarp();
+    if (sent < boxes) send();
+    if (row + kBoxRows >= len) w.finish(p, q_row, p.c.group);
+  }
+  if (!alive && lane == 0)  // no warp leaves under a copy of its own
+    for (int i = max(0, sent - S::kStages); i < sent; ++i)
+      wait_bar(smem_u32(&sh.full_own[i % S::kStages][warp]), (i / S::kStages) & 1, &sh.ctl, p.status, false);
+}
+
+// The partial results of a portion's CTAs, joined in their order, by the consumer warps of the CTA that came last.
+// The ring, which is at rest, takes them: all that fits is on its way at once, since a load takes 2 us while others use
+// the memory.
+template <int D, bool BF16, int Q>
+__device__ __forceinline__ void join_parts(const PageParams& p, const Pending& x, unsigned char* ring_mem) {
+  using S = Shape<D, BF16, Q>;
+  const int tid = threadIdx.x, n = x.n, queries = x.queries;
+  const auto slot = [&](int i) { return (size_t)(x.w0 + i) * 2 + (i == 0); };  // (there the last, then the first portion)
+  float2* const ml = reinterpret_cast<float2*>(ring_mem);                      // [query][part]
+  const int head_bytes = (queries * n * 8 + 15) / 16 * 16, row_bytes = queries * D * 4;
+  unsigned char* const rows = ring_mem + head_bytes;
+  const int fit = (S::kStages * S::kStageBytes - head_bytes) / row_bytes;      // parts at a time
+  meet();  // (a join before this one is through with the ring)
+  float4 acc[Q * D / 4 / (kConsumers * 32) + 1];
+#pragma unroll
+  for (int j = 0; j < (int)(sizeof(acc) / sizeof(acc[0])); ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = 0; i0 < n; i0 += fit) {
+    const int cnt = min(fit, n - i0);
+    if (i0 > 0) meet();
+    for (int i = 0; i < cnt; ++i) {
+      const char* from = reinterpret_cast<const char*>(p.part + slot(i0 + i) * Q * D);
+      for (int at = tid * 16; at < row_bytes; at += kConsumers * 32 * 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(rows + i * row_bytes + at)),
+                     "l"(from + at) : "memory");
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (i0 == 0) {
+      for (int e = tid; e < n * queries; e += kConsumers * 32) {
+        const int i = e / queries, q = e - i * queries;
+        ml[q * n + i] = __ldcg(p.part_ml + slot(i) * Q + q);
+      }
+      meet();
+      // maxima to weights; the weighted sum of the sums in front
+      for (int q = tid >> 5; q < queries; q += kConsumers) {
+        const int lane = tid & 31;
+        float top = -INFINITY, l = 0.f;
+        for (int i = lane; i < n; i += 32) top = fmaxf(top, ml[q * n + i].x);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        for (int i = lane; i < n; i += 32) {
+          const float e = fast_exp2(ml[q * n + i].x - finite_ref(top));
+          l = fmaf(e, ml[q * n + i].y, l);
+          ml[q * n + i].x = e;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        __syncwarp();
+        if (lane == 0) {
+          ml[q * n].y = l;
+          if (p.lse) p.lse[x.q_row + q] = (top + fast_log2(l)) * kLn2;
+        }
+      }
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    meet();
+#pragma unroll
+    for (int j = 0; j < (int)(sizeof(acc) / sizeof(acc[0])); ++j) {
+      const int e = tid + j * kConsumers * 32;
+      if (e >= queries * (D / 4)) break;
+      const int q = e / (D / 4);
+#pragma unroll 4
+      for (int i = 0; i < cnt; ++i) {
+        const float w = ml[q * n + i0 + i].x;
+        const float4 f = *reinterpret_cast<const float4*>(rows + (size_t)i * row_bytes + e * 16);
+        acc[j] = make_float4(fmaf(w, f.x, acc[j].x), fmaf(w, f.y, acc[j].y), fmaf(w, f.z, acc[j].z), fmaf(w, f.w, acc[j].w));
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < (int)(sizeof(acc) / sizeof(acc[0])); ++j) {
+    const int e = tid + j * kConsumers * 32;
+    if (e >= queries * (D / 4)) break;
+    const int q = e / (D / 4);
+    const float l = ml[q * n].y;
+    store4<BF16>(p.out, (x.q_row + q) * D + e % (D / 4) * 4, make_float4(acc[j].x / l, acc[j].y / l, acc[j].z / l, acc[j].w / l));
+  }
+  if (tid == 0) p.counters[x.w0] = 0;  // ready for the next call
+}
 
 template <int D, bool BF16, int Q>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                     const __grid_constant__ PageParams p) {
   using S = Shape<D, BF16, Q>;
-  using Warp = typename std::conditional<BF16, TensorWarp<D, Q>, PlainWarp<D, Q>>::type;
+  using Warp = WarpOf<D, BF16, Q>;
   constexpr int kWarpsAll = kThreads / 32;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(8) uint64_t full_k[S::kStages], full_v[S::kStages], empty[S::kStages];
-  __shared__ Ctl ctl;
-  __shared__ int issued, last_one[2];
-  __shared__ Start start;
-  __shared__ int cuts[kConsumers + 1], cut_at[kConsumers + 1];  // by warp: their first heads, and boxes before those
-  __shared__ Counts sums[kWarpsAll];
-  __shared__ float2 stats[kConsumers][Q];
-  __shared__ __align__(16) float q_mem[BF16 ? 4 : (Warp::kOwnQueries ? kConsumers : 1) * Q * D];  // fp32: the queries
-  __shared__ __align__(16) float prob_mem[BF16 ? 4 : kConsumers * S::kWarpRows * Q];
+  __shared__ Shared<D, BF16, Q> sh;
   const Cache& c = p.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  unsigned char* const ring_mem = smem_raw + (ring - smem_u32(smem_raw));
 
   if (tid == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k));
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v));
     for (int s = 0; s < S::kStages; ++s) {
-      mbar_init(smem_u32(&full_k[s]), 1);
-      mbar_init(smem_u32(&full_v[s]), 1);
-      mbar_init(smem_u32(&empty[s]), kConsumers);
+      mbar_init(smem_u32(&sh.full[s]), 1);
+      mbar_init(smem_u32(&sh.empty[s]), kConsumers);
+      for (int w = 0; w < kConsumers; ++w) mbar_init(smem_u32(&sh.full_own[s][w]), 1);
     }
-    ctl.abort_flag = 0;
-    ctl.wait_cycles = p.wait_cycles;
-    issued = 0;
+    sh.ctl.abort_flag = 0;
+    sh.ctl.wait_cycles = p.wait_cycles;
+    sh.issued = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   in_stream_order();
 
-  // ---- the cut, and this CTA's part -----------------------------------------------------------------
-  Plan plan;
-  long long at0 = 0, at1 = 0;
-  {
-    const int share = (p.heads + kThreads - 1) / kThreads;
-    const int h0 = min(p.heads, tid * share), h1 = min(p.heads, h0 + share);
-    Counts mine = {};
-#pragma unroll 4
-    for (int h = h0; h < h1; ++h) {
-      const int len = head_len(p, h);
-      const int tiles = tiles_of<S>(len), boxes = (len + kBoxRows - 1) / kBoxRows;
-      mine.add({tiles, boxes, (tiles + S::kSmall - 1) / S::kSmall, (tiles + S::kLarge - 1) / S::kLarge, boxes});
-      if (len == 0 && h % (int)gridDim.x == (int)blockIdx.x) {  // no rows: zeros
-        const int prob = h / c.n_kv_heads, kvh = h - prob * c.n_kv_heads;
-        const size_t row = (size_t)prob * c.n_q_heads + (size_t)kvh * c.group;
-        for (int i = 0; i < c.group * D; i += 4) store4<BF16>(p.out, row * D + i, make_float4(0.f, 0.f, 0.f, 0.f));
-        if (p.lse)
-          for (int i = 0; i < c.group; ++i) p.lse[row + i] = -INFINITY;
-      }
+  // ---- the cut: segments of heads are counted, a warp each; every warp finds what it needs ----------
+  int seg_heads = 32;  // a power of two
+  while (seg_heads * kSegs < p.heads) seg_heads *= 2;
+  if (p.heads <= 32 * kWarpsAll) {  // (little code: it is fetched anew by every launch)
+    const int h = 32 * warp + lane;
+    if (32 * warp < p.heads) {
+      const Counts sum = (h < p.heads ? Counts::of<S>(head_len(p, h)) : Counts{}).over_warp();
+      if (lane == 0) sh.segs[warp] = sum;
     }
-    const Counts of_warp = {__reduce_add_sync(0xffffffffu, mine.tiles), __reduce_add_sync(0xffffffffu, mine.boxes),
-                            __reduce_add_sync(0xffffffffu, mine.small), __reduce_add_sync(0xffffffffu, mine.large),
-                            __reduce_max_sync(0xffffffffu, mine.most)};
-    if (lane == 0) sums[warp] = of_warp;
-    __syncthreads();
-    Counts all = {}, warps_before = {};
-    for (int w = 0; w < kWarpsAll; ++w) {
-      if (w == warp) warps_before = all;
-      all.add(sums[w]);
-    }
-    plan = plan_of<S>(p, all);
-    if ((int)blockIdx.x >= plan.parts) return;
-    // what the cut counts, up to this thread's heads and in them
-    const auto counted = [&](const Counts& x) {
-      return plan.by_warp ? x.boxes : plan.piece == S::kSmall ? x.small : plan.piece ? x.large : x.tiles;
-    };
-    const int here = counted(mine);
-    int incl = here;
+  } else {
+    const int span = max(512, seg_heads), per_seg = seg_heads / 32;
+    for (int h0 = warp * span; h0 < p.heads; h0 += kWarpsAll * span) {
+      Counts mine = {};
+      for (int i = h0; i < h0 + span; i += 512) {
+        int len[16];  // sixteen loads at once
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += y;
-    }
-    const int before = counted(warps_before) + incl - here;
-    if (plan.by_warp) {
-      const long long workers = (long long)gridDim.x * kConsumers;
-      for (int k = 0; k <= kConsumers; ++k) {  // the first head whose boxes begin at the cut or behind it
-        const int cut = (int)(all.boxes * ((long long)blockIdx.x * kConsumers + k) / workers);
-        if (cut == 0 && tid == 0) cuts[k] = cut_at[k] = 0;
-        if (before < cut && cut <= before + here) {
-          int at = before, h = h0;
-          for (; at < cut; ++h) at += (head_len(p, h) + kBoxRows - 1) / kBoxRows;
-          cuts[k] = h;
-          cut_at[k] = at;
+        for (int j = 0; j < 16; ++j) {
+          const int h = i + 32 * j + lane;
+          len[j] = h < p.heads ? head_len(p, h) : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          if (len[j] >= 0) mine.add(Counts::of<S>(len[j]));
+          const int h = i + 32 * j;
+          if (((h / 32 + 1) & (per_seg - 1)) == 0) {
+            const Counts sum = mine.over_warp();
+            if (lane == 0 && h - (seg_heads - 32) < p.heads) sh.segs[h / seg_heads] = sum;
+            mine = Counts{};
+          }
         }
       }
-    } else {
-      // the unit of the line, a tile or a piece, that this CTA's part begins with
-      at0 = plan.piece ? (long long)blockIdx.x : plan.total * blockIdx.x / plan.parts;
-      at1 = plan.total * (blockIdx.x + 1ll) / plan.parts;
-      const long long first = (long long)before * p.subs;
-      if (at0 >= first && at0 < first + (long long)here * p.subs) {
-        const int size = plan.piece ? plan.piece : 1;
-        const auto units = [&](int h) { return (tiles_of<S>(head_len(p, h)) + size - 1) / size; };
-        long long at = first;
-        int h = h0, n = units(h);
-        while (at + (long long)n * p.subs <= at0) {
-          at += (long long)n * p.subs;
-          n = units(++h);
-        }
-        const int sub = (int)((at0 - at) / n), i = (int)((at0 - at) % n);
-        const long long tiles = tiles_of<S>(head_len(p, h));
-        if (plan.piece)
-          start = {h, sub, (int)(tiles * i / n), (int)(tiles * (i + 1) / n), (int)at0 - i, n};
-        else
-          start = {h, sub, i, 0, 0, 0};
-      }
     }
-    __syncthreads();
   }
-  int stage = 0, use = 0;
-  bool alive = true;
+  __syncthreads();
+  Counts all = {};
+  for (int seg = lane; seg * seg_heads < p.heads; seg += 32) all.add(sh.segs[seg]);
+  all = all.over_warp();
+  if (all.empty)  // zeros for heads without rows
+    for (int h = blockIdx.x + tid * gridDim.x; h < p.heads; h += kThreads * gridDim.x) {
+      if (head_len(p, h) > 0) continue;
+      const size_t row = first_query(c, h);
+      for (int e = 0; e < c.group * D; e += 4) store4<BF16>(p.out, row * D + e, make_float4(0.f, 0.f, 0.f, 0.f));
+      if (p.lse)
+        for (int e = 0; e < c.group; ++e) p.lse[row + e] = -INFINITY;
+    }
+  const Plan plan = plan_of<S>(p, all);
+  if ((int)blockIdx.x >= plan.parts) return;
+
+  if (plan.by_warp) {
+    if constexpr (S::kWarpRows == kBoxRows && Warp::kOwnQueries) {
+      if (warp == kConsumers) return;
+      // the heads whose first box is in this warp's part of all boxes
+      const int workers = plan.parts * kConsumers, i = blockIdx.x * kConsumers + warp;
+      int begin[2], at[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int cut = part_begin(all.boxes, workers, i + k);
+        const int2 f = find_unit<S>(p, sh.segs, seg_heads, cut, [](const Counts& x) { return x.boxes; });
+        begin[k] = f.x;
+        at[k] = f.y;
+        if (f.y < cut && f.x < p.heads) {  // inside a head: the next one
+          at[k] += Counts::of<S>(head_len(p, f.x)).boxes;
+          ++begin[k];
+        }
+      }
+      whole_heads(p, &map_k, &map_v, sh, ring, begin[0], begin[1], at[1] - at[0]);
+    }
+    return;
+  }
+  Part part;
+  {
+    const int unit = plan.piece ? (int)blockIdx.x : part_begin(plan.total, plan.parts, blockIdx.x);
+    const auto counted = [&](const Counts& x) {
+      return (plan.piece == S::kSmall ? x.small : plan.piece ? x.large : x.tiles) * p.subs;
+    };
+    const int2 f = find_unit<S>(p, sh.segs, seg_heads, unit, counted);
+    const Counts its = Counts::of<S>(head_len(p, f.x));
+    const int tiles = its.tiles, n = plan.piece == S::kSmall ? its.small : plan.piece ? its.large : tiles;
+    const int sub = p.subs == 1 ? 0 : (unit - f.y) / n, i = unit - f.y - sub * n;
+    part.head = f.x;
+    part.sub = sub;
+    if (plan.piece) {
+      part.tile = n == 1 ? 0 : part_begin(tiles, n, i);
+      part.tiles = n == 1 ? tiles : part_begin(tiles, n, i + 1) - part.tile;
+      part.first = unit - i;
+      part.pieces = n;
+    } else {
+      part.tile = i;
+      part.tiles = part_begin(plan.total, plan.parts, blockIdx.x + 1) - unit;
+      part.first = part.pieces = 0;
+    }
+  }
   const auto wait = [&](uint64_t* bar, int parity) {  // the same in all lanes
-    return __all_sync(0xffffffffu, wait_bar(smem_u32(bar), parity, &ctl, p.status)) != 0;
+    return __all_sync(0xffffffffu, wait_bar(smem_u32(bar), parity, &sh.ctl, p.status)) != 0;
   };
+  int stage = 0, parity = 0;
   const auto next_stage = [&] {
     if (++stage == S::kStages) {
       stage = 0;
-      ++use;
+      parity ^= 1;
     }
   };
-  // first row of the pool that a box of rows `row` ... is in (a page that is none of the pool: behind the pool's
-  // rows, where copies give zeros)
-  const auto place = [&](int h, int row) {
-    const int page = p.table[(size_t)(p.first_head + h) * c.max_pages + (row >> c.page_shift)];
-    return (unsigned)page < (unsigned)c.n_pages ? (page << c.page_shift) + (row & (c.page_rows - 1))
-                                                : c.n_pages << c.page_shift;
-  };
+  int h = part.head, sub = part.sub, t0 = part.tile, done = 0;  // t0: of the portion in hand; done: tiles of the part
 
-  if (plan.by_warp) {
-    if constexpr (S::kWarpRows == kBoxRows) {
-      int stages = 0;  // as many as the warp with most boxes has
-#pragma unroll
-      for (int k = 0; k < kConsumers; ++k) stages = max(stages, cut_at[k + 1] - cut_at[k]);
-      if (warp == kConsumers) {
-        // ---- producer: lanes 2 i and 2 i + 1 walk the heads of warp i, for K and for V; box i of a stage is warp i's
-        const int of = min(lane >> 1, kConsumers - 1);
-        const bool v = lane & 1, walks = lane < 2 * kConsumers;
-        int h = cuts[of], end = walks ? cuts[of + 1] : 0, row = 0, len = 0;
-        const auto advance = [&] {  // to the next row that begins a box, in a head that has rows
-          while (h < end && row >= len) {
-            if (len > 0) ++h;
-            len = h < end ? head_len(p, h) : 0;
-            row = 0;
-            if (len == 0 && h < end) ++h;
-          }
-        };
-        advance();
-        int at = h < end ? place(h, row) : 0;
-        for (; stages > 0; --stages) {
-          if (use > 0 && !(alive = wait(&empty[stage], (use - 1) & 1))) break;
-          const int boxes = __popc(__ballot_sync(0xffffffffu, h < end)) / 2;
-          if (lane == 0) {
-            mbar_expect_tx(smem_u32(&full_k[stage]), boxes * S::kBoxBytes);
-            mbar_expect_tx(smem_u32(&full_v[stage]), boxes * S::kBoxBytes);
-            ++issued;
-          }
-          __syncwarp();
-          if (h < end) {
-            tma_load_3d(ring + stage * S::kStageBytes + (v ? S::kTileBytes : 0) + of * S::kBoxBytes, v ? &map_v : &map_k, 0,
-                        at, 0, smem_u32(v ? &full_v[stage] : &full_k[stage]));
-            row += kBoxRows;
-            advance();
-            if (h < end) at = place(h, row);
-          }
-          next_stage();
-          __syncwarp();
-        }
-      } else {
-        // ---- consumers: their own heads
-        Warp w;
-        const Logit logit(c);
-        float* const probs = prob_mem + (BF16 ? 0 : warp * S::kWarpRows * Q);
-        for (int h = cuts[warp]; h < cuts[warp + 1] && alive; ++h) {
-          const int len = head_len(p, h);
-          if (len == 0) continue;
-          const int prob = h / c.n_kv_heads, kvh = h - prob * c.n_kv_heads;
-          const size_t q_row = (size_t)prob * c.n_q_heads + (size_t)kvh * c.group;
-          if constexpr (BF16) w.begin(p, q_row, c.group);
-          else w.begin(p, q_row, c.group, q_mem + warp * Q * D);
-          for (int row = 0; row < len; row += kBoxRows) {
-            const uint32_t k_tile = ring + stage * S::kStageBytes;
-            if (!(alive = wait(&full_k[stage], use & 1))) break;
-            alive = w.tile(k_tile, k_tile + S::kTileBytes, warp * kBoxRows, min(kBoxRows, len - row), logit, probs,
-                           [&] { return wait(&full_v[stage], use & 1); });
-            if (!alive) break;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
-            next_stage();
-            --stages;
-          }
-          if (alive) w.finish(p, q_row, c.group);
-        }
-        for (; stages > 0 && alive; --stages) {  // with boxes of other warps only
-          alive = wait(&full_k[stage], use & 1);
-          if (alive && lane == 0) mbar_arrive(smem_u32(&empty[stage]));
-          next_stage();
-        }
-      }
-    }
-  } else if (warp == kConsumers) {
+  if (warp == kConsumers) {
     // ---- producer ----------------------------------------------------------------------------------
-    long long left = plan.piece ? start.end - start.tile : at1 - at0;
-    int sub = start.sub, t0 = start.tile;  // of the head in hand; 0 in the heads that follow
-    for (int h = start.head; left > 0 && alive; ++h, sub = 0) {
+    constexpr int kBoxes = S::kTile / kBoxRows, kAhead = 32 / kBoxes;
+    bool alive = true;
+    for (; done < part.tiles && alive; ++h, sub = 0) {
       const int len = head_len(p, h), n = tiles_of<S>(len);
       if (n == 0) continue;
-      for (; sub < p.subs && left > 0 && alive; ++sub, t0 = 0) {
-        const int t1 = (int)min((long long)n, t0 + left);
-        left -= t1 - t0;
-        for (int t = t0; t < t1; ++t) {
-          const int row0 = t * S::kTile;
-          const int boxes = min(S::kTile / kBoxRows, (len - row0 + kBoxRows - 1) / kBoxRows);
+      for (; sub < p.subs && done < part.tiles && alive; ++sub, t0 = 0) {
+        const int tiles = min(n - t0, part.tiles - done);
+        int places = 0;
+        for (int t = 0; t < tiles; ++t) {
+          if (t % kAhead == 0) {  // the places of the next 32 boxes, a lane each
+            const int row = (t0 + t) * S::kTile + lane * kBoxRows;
+            places = row < len ? place(p, h, row) : 0;
+          }
+          const int boxes = min(kBoxes, (len - (t0 + t) * S::kTile + kBoxRows - 1) / kBoxRows);
           // lane 2 i + v: box i of K or V
-          const int at = lane < 2 * boxes ? place(h, row0 + (lane >> 1) * kBoxRows) : 0;
-          if (use > 0 && !(alive = wait(&empty[stage], (use - 1) & 1))) break;
+          const int at = __shfl_sync(0xffffffffu, places, t % kAhead * kBoxes + (lane >> 1) % kBoxes);
+          if (done + t >= S::kStages && !(alive = wait(&sh.empty[stage], parity ^ 1))) break;
           if (lane == 0) {
-            mbar_expect_tx(smem_u32(&full_k[stage]), boxes * S::kBoxBytes);
-            mbar_expect_tx(smem_u32(&full_v[stage]), boxes * S::kBoxBytes);
-            ++issued;
+            mbar_expect_tx(smem_u32(&sh.full[stage]), 2 * boxes * S::kBoxBytes);
+            ++sh.issued;
           }
           __syncwarp();
           if (lane < 2 * boxes) {
             const bool v = lane & 1;
             tma_load_3d(ring + stage * S::kStageBytes + (v ? S::kTileBytes : 0) + (lane >> 1) * S::kBoxBytes,
-                        v ? &map_v : &map_k, 0, at, 0, smem_u32(v ? &full_v[stage] : &full_k[stage]));
+                        v ? &map_v : &map_k, 0, at, 0, smem_u32(&sh.full[stage]));
           }
           next_stage();
         }
+        done += tiles;
       }
     }
   } else {
     // ---- consumers ---------------------------------------------------------------------------------
     Warp w;
     const Logit logit(c);
-    float* const probs = prob_mem + (BF16 ? 0 : warp * S::kWarpRows * Q);
-    Pending begun = {}, ended = {};  // the portion that the part begins in, and the one that it ends in
-    long long left = plan.piece ? start.end - start.tile : at1 - at0;
-    int sub = start.sub, t0 = start.tile;
-    long long at = at0 - t0;  // first tile of the head's portion on the line
-    for (int h = start.head; left > 0 && alive; ++h, sub = 0) {
+    unsigned char* const q_mem = sh.q_mem[Warp::kOwnQueries ? warp : 0];
+    float* const probs = sh.probs[BF16 ? 0 : warp];
+    int fetched = -1;  // the head whose queries are on their way
+    bool alive = true, begun = false, ended = false;  // others have tiles of the portion that the part begins, ends in
+    for (; done < part.tiles && alive; ++h, sub = 0) {
       const int len = head_len(p, h), n = tiles_of<S>(len);
       if (n == 0) continue;
-      const int prob = h / c.n_kv_heads, kvh = h - prob * c.n_kv_heads;
-      for (; sub < p.subs && left > 0; ++sub, t0 = 0) {
-        const int t1 = (int)min((long long)n, t0 + left);
-        const int queries = min(p.per_sub, c.group - sub * p.per_sub);
-        const size_t q_row = (size_t)prob * c.n_q_heads + (size_t)kvh * c.group + sub * p.per_sub;
-        if constexpr (BF16) w.begin(p, q_row, queries);
-        else w.begin(p, q_row, queries, q_mem + (Warp::kOwnQueries ? warp * Q * D : 0));
-        for (int t = t0; t < t1; ++t) {
-          const uint32_t k_tile = ring + stage * S::kStageBytes, v_tile = k_tile + S::kTileBytes;
-          const int r0 = warp * S::kWarpRows, valid = min(S::kWarpRows, len - t * S::kTile - r0);
-          if (!(alive = wait(&full_k[stage], use & 1))) break;
-          const auto v_ready = [&] { return wait(&full_v[stage], use & 1); };
-          alive = valid > 0 ? w.tile(k_tile, v_tile, r0, valid, logit, probs, v_ready) : v_ready();
-          if (!alive) break;
-          if (t + 1 < t1) {  // (the last stage is kept for the meeting)
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
-            next_stage();
-          }
+      for (; sub < p.subs && done < part.tiles; ++sub, t0 = 0) {
+        const int tiles = min(n - t0, part.tiles - done), queries = min(p.per_sub, c.group - sub * p.per_sub);
+        if (fetched != h) w.fetch(p, first_query(c, h) + sub * p.per_sub, queries);
+        w.begin(q_mem);
+        if (p.subs == 1) {  // the next head's, in case it follows
+          fetched = min(h + 1, p.heads - 1);
+          w.fetch(p, first_query(c, fetched), queries);
         }
-        // The warps meet: each leaves its maxima and sums, and what it has summed of V in the memory of its own rows
-        // of the last stage, which no other warp reads.
-        unsigned char* const last = smem_raw + (ring - smem_u32(smem_raw)) + stage * S::kStageBytes;
-        w.leave_stats(stats[warp]);
+        int valid = len - t0 * S::kTile - warp * S::kWarpRows;  // rows from this warp's first one on
+        for (int t = 0;; ++t, valid -= S::kTile) {
+          const uint32_t k_tile = ring + stage * S::kStageBytes;
+          if (!(alive = wait(&sh.full[stage], parity))) break;
+          if (valid > 0)
+            w.tile(k_tile, k_tile + S::kTileBytes, warp * S::kWarpRows, min(S::kWarpRows, valid), logit, q_mem, probs);
+          if (t + 1 == tiles) break;  // (the last stage is kept for the meeting)
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&sh.empty[stage]));
+          next_stage();
+        }
+        // The warps meet: each leaves its maxima and sums, and what it has summed of V in the memory of its own rows of
+        // the last stage, which no other warp reads.
+        unsigned char* const last = ring_mem + stage * S::kStageBytes;
+        w.leave_stats(sh.stats[warp]);
         __syncwarp();
         w.leave_sums(last, warp);
         alive = meet_all(alive);
         if (!alive) break;
-        const bool whole = t0 == 0 && t1 == n;
+        const size_t q_row = first_query(c, h) + sub * p.per_sub;
+        const bool whole = tiles == n;
         const size_t slot = (size_t)blockIdx.x * 2 + (t0 == 0);
         for (int e = tid; e < queries * (D / 4); e += kConsumers * 32) {
           const int q = e / (D / 4), col = e % (D / 4) * 4;
-          const float top = top_of<Q>(stats, q);
+          const float top = top_of<Q>(sh.stats, q);
           float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
           float l = 0.f;
 #pragma unroll
           for (int i = 0; i < kConsumers; ++i) {
             const float4 f = *reinterpret_cast<const float4*>(last + Warp::sum_at(i, q, col));
-            const float s = fast_exp2(stats[i][q].x - finite_ref(top));
-            a = make_float4(fmaf(f.x, s, a.x), fmaf(f.y, s, a.y), fmaf(f.z, s, a.z), fmaf(f.w, s, a.w));
-            l = fmaf(stats[i][q].y, s, l);
+            const float x = fast_exp2(sh.stats[i][q].x - finite_ref(top));
+            a = make_float4(fmaf(f.x, x, a.x), fmaf(f.y, x, a.y), fmaf(f.z, x, a.z), fmaf(f.w, x, a.w));
+            l = fmaf(sh.stats[i][q].y, x, l);
           }
           if (whole) {
             store4<BF16>(p.out, (q_row + q) * D + col, make_float4(a.x / l, a.y / l, a.z / l, a.w / l));
@@ -823,48 +1010,43 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             if (col == 0) p.part_ml[slot * Q + q] = make_float2(top, l);
           }
         }
+        if (!whole) {
+          if (t0 == 0) ended = true;
+          else begun = true;
+          if (tid == 0) {  // the CTAs that have tiles of the portion
+            Pending x = {part.first, part.pieces, queries, q_row};
+            if (!plan.piece) {
+              const int at = part_begin(plan.total, plan.parts, blockIdx.x) + done - t0;  // the portion's first tile
+              x.w0 = part_of(plan.total, plan.parts, at);
+              x.n = part_of(plan.total, plan.parts, at + n - 1) + 1 - x.w0;
+            }
+            sh.pending[t0 == 0] = x;
+          }
+        }
         fence_async_proxy();  // (the stage was written; the next copy into it comes after)
         meet();
-        if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
+        if (lane == 0) mbar_arrive(smem_u32(&sh.empty[stage]));
         next_stage();
-        if (!whole) {
-          // the parts that the portion's tiles lie in
-          Pending x = {start.first, start.pieces, queries, q_row};
-          if (!plan.piece) {
-            x.w0 = (int)(((at + 1) * plan.parts - 1) / plan.total);
-            x.n = (int)(((at + n) * plan.parts - 1) / plan.total) + 1 - x.w0;
-          }
-          if (t0 == 0) ended = x;
-          else begun = x;
-        }
-        left -= t1 - t0;
-        at += n;
+        done += tiles;
       }
     }
-    // Portions that other CTAs have parts of, when this CTA is through: who comes last joins them.
-    if (alive && (begun.n || ended.n)) {
+    // Portions that other CTAs have tiles of, when the part is through: who comes last joins them.
+    if (alive && (begun || ended)) {
       __threadfence();
       meet();
-      if (tid == 0 && begun.n) last_one[0] = atomicAdd(p.counters + begun.w0, 1) == begun.n - 1;
-      if (tid == 32 && ended.n) last_one[1] = atomicAdd(p.counters + ended.w0, 1) == ended.n - 1;
+      if (tid == 0 && begun) sh.last_one[0] = atomicAdd(p.counters + sh.pending[0].w0, 1) == sh.pending[0].n - 1;
+      if (tid == 32 && ended) sh.last_one[1] = atomicAdd(p.counters + sh.pending[1].w0, 1) == sh.pending[1].n - 1;
       meet();
       __threadfence();
-      if (begun.n && last_one[0]) {
-        join_parts<D, BF16, Q>(p, begun.w0, begun.n, begun.queries, begun.q_row);
-        if (tid == 0) p.counters[begun.w0] = 0;
-      }
-      if (ended.n && last_one[1]) {
-        join_parts<D, BF16, Q>(p, ended.w0, ended.n, ended.queries, ended.q_row);
-        if (tid == 0) p.counters[ended.w0] = 0;
-      }
+      for (int i = begun ? 0 : 1; i < (ended ? 2 : 1); ++i)
+        if (sh.last_one[i]) join_parts<D, BF16, Q>(p, sh.pending[i], ring_mem);
     }
   }
   // after a wait that gave up: no CTA leaves under a copy of its own
   __syncthreads();
-  if (ctl.abort_flag && tid == 0) {
-    for (int i = max(0, issued - S::kStages); i < issued; ++i) {
-      wait_bar(smem_u32(&full_k[i % S::kStages]), (i / S::kStages) & 1, &ctl, p.status, false);
-      wait_bar(smem_u32(&full_v[i % S::kStages]), (i / S::kStages) & 1, &ctl, p.status, false);
+  if (sh.ctl.abort_flag && tid == 0) {
+    for (int i = max(0, sh.issued - S::kStages); i < sh.issued; ++i) {
+      wait_bar(smem_u32(&sh.full[i % S::kStages]), (i / S::kStages) & 1, &sh.ctl, p.status, false);
     }
   }
 }
@@ -894,6 +1076,7 @@ lava_status launch(const CUtensorMap& map_k, const CUtensorMap& map_v, PageParam
   if (rc != LAVA_OK) return rc;
   const long long most = ((((long long)p.c.max_pages << p.c.page_shift) + S::kTile - 1) / S::kTile) * p.heads * p.subs;
   const int grid = (int)std::min<long long>(most_ctas(), most);
+  p.own_queries = WarpOf<D, BF16, Q>::kOwnQueries;
   const cudaError_t e = launch_in_order(kernel, grid, kThreads, S::kSmem, stream, map_k, map_v, p);
   count_launches(1);
   return check_cuda(e, "paged decode attention launch");
@@ -928,19 +1111,20 @@ lava_status lava_decode_attention_pages(const lava_cache_desc* cache, int32_t fi
     return fail(LAVA_ERR_INVALID_ARG, "NULL argument");
   if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out))
     return fail(LAVA_ERR_INVALID_ARG, "q, k_pages, v_pages and out must be 16-byte aligned");
-  if (((long long)n_layers * c.batch * c.n_kv_heads) >= (1ll << 35) / ((long long)c.max_pages << c.page_shift))
-    return fail(LAVA_ERR_UNSUPPORTED, "the heads of the call times the rows of a head must stay below 2^35");
   const size_t need = lava_cache_workspace_bytes(cache);
   if (!workspace || workspace_bytes < need)
     return fail(LAVA_ERR_WORKSPACE, "workspace too small: %zu < %zu bytes", workspace_bytes, need);
   if (!aligned16(workspace)) return fail(LAVA_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+  const Portions portions = portions_of(c);
+  if ((long long)n_layers * c.batch * c.n_kv_heads * portions.subs >= (1ll << 35) / ((long long)c.max_pages << c.page_shift))
+    return fail(LAVA_ERR_UNSUPPORTED, "too many rows in one call: heads * max_pages * page_rows must stay below 2^35");
   CUtensorMap map_k, map_v;
   rc = encode_pages_map(c, k_pages, &map_k);
   if (rc == LAVA_OK) rc = encode_pages_map(c, v_pages, &map_v);
   if (rc != LAVA_OK) return rc;
-  const Portions portions = portions_of(c);
   p.first_head = first_layer * c.batch * c.n_kv_heads;
   p.heads = n_layers * c.batch * c.n_kv_heads;
+  p.queries = p.heads * c.group;
   p.subs = portions.subs;
   p.per_sub = portions.per_sub;
   p.q = q;
