@@ -539,7 +539,7 @@ template <int D, bool BF16, int Q>
 struct Shared {
   using S = Shape<D, BF16, Q>;
   using Warp = WarpOf<D, BF16, Q>;
-  uint64_t full[S::kStages], empty[S::kStages];
+  uint64_t full[S::kStages], empty[S::kStages], joined;
   uint64_t full_own[S::kStages][kConsumers];           // by warp: of its box of a stage
   Ctl ctl;
   int issued, last_one[2];
@@ -707,7 +707,8 @@ __device__ __forceinline__ void whole_heads(const PageParams& p, const CUtensorM
 // The ring, which is at rest, takes them: all that fits is on its way at once, since a load takes 2 us while others use
 // the memory.
 template <int D, bool BF16, int Q>
-__device__ __forceinline__ void join_parts(const PageParams& p, const Pending& x, unsigned char* ring_mem) {
+__device__ __forceinline__ bool join_parts(const PageParams& p, Shared<D, BF16, Q>& sh, const Pending& x,
+                                           unsigned char* ring_mem, int& turn) {
   using S = Shape<D, BF16, Q>;
   const int tid = threadIdx.x, n = x.n, queries = x.queries;
   const auto slot = [&](int i) { return (size_t)(x.w0 + i) * 2 + (i == 0); };  // (there the last, then the first portion)
@@ -715,20 +716,23 @@ __device__ __forceinline__ void join_parts(const PageParams& p, const Pending& x
   const int head_bytes = (queries * n * 8 + 15) / 16 * 16, row_bytes = queries * D * 4;
   unsigned char* const rows = ring_mem + head_bytes;
   const int fit = (S::kStages * S::kStageBytes - head_bytes) / row_bytes;      // parts at a time
-  meet();  // (a join before this one is through with the ring)
+  // (the partial results and what the ring held before are there for the copies that follow)
+  asm volatile("fence.proxy.async;" ::: "memory");
+  meet();
   float4 acc[Q * D / 4 / (kConsumers * 32) + 1];
 #pragma unroll
   for (int j = 0; j < (int)(sizeof(acc) / sizeof(acc[0])); ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i0 = 0; i0 < n; i0 += fit) {
     const int cnt = min(fit, n - i0);
     if (i0 > 0) meet();
-    for (int i = 0; i < cnt; ++i) {
-      const char* from = reinterpret_cast<const char*>(p.part + slot(i0 + i) * Q * D);
-      for (int at = tid * 16; at < row_bytes; at += kConsumers * 32 * 16)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(rows + i * row_bytes + at)),
-                     "l"(from + at) : "memory");
+    if (tid < 32) {
+      if (tid == 0) mbar_expect_tx(smem_u32(&sh.joined), cnt * row_bytes);
+      __syncwarp();
+      for (int i = tid; i < cnt; i += 32)
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                     ::"r"(smem_u32(rows + i * row_bytes)), "l"(p.part + slot(i0 + i) * Q * D), "r"(row_bytes),
+                       "r"(smem_u32(&sh.joined)) : "memory");
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
     if (i0 == 0) {
       for (int e = tid; e < n * queries; e += kConsumers * 32) {
         const int i = e / queries, q = e - i * queries;
@@ -756,8 +760,7 @@ __device__ __forceinline__ void join_parts(const PageParams& p, const Pending& x
         }
       }
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    meet();
+    if (!meet_all(wait_bar(smem_u32(&sh.joined), turn++ & 1, &sh.ctl, p.status, false))) return false;
 #pragma unroll
     for (int j = 0; j < (int)(sizeof(acc) / sizeof(acc[0])); ++j) {
       const int e = tid + j * kConsumers * 32;
@@ -780,6 +783,7 @@ __device__ __forceinline__ void join_parts(const PageParams& p, const Pending& x
     store4<BF16>(p.out, (x.q_row + q) * D + e % (D / 4) * 4, make_float4(acc[j].x / l, acc[j].y / l, acc[j].z / l, acc[j].w / l));
   }
   if (tid == 0) p.counters[x.w0] = 0;  // ready for the next call
+  return true;
 }
 
 template <int D, bool BF16, int Q>
@@ -804,6 +808,7 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
       mbar_init(smem_u32(&sh.empty[s]), kConsumers);
       for (int w = 0; w < kConsumers; ++w) mbar_init(smem_u32(&sh.full_own[s][w]), 1);
     }
+    mbar_init(smem_u32(&sh.joined), 1);
     sh.ctl.abort_flag = 0;
     sh.ctl.wait_cycles = p.wait_cycles;
     sh.issued = 0;
@@ -1032,14 +1037,16 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     }
     // Portions that other CTAs have tiles of, when the part is through: who comes last joins them.
     if (alive && (begun || ended)) {
+      asm volatile("fence.proxy.async;" ::: "memory");  // (bulk copies will read the partial results)
       __threadfence();
       meet();
       if (tid == 0 && begun) sh.last_one[0] = atomicAdd(p.counters + sh.pending[0].w0, 1) == sh.pending[0].n - 1;
       if (tid == 32 && ended) sh.last_one[1] = atomicAdd(p.counters + sh.pending[1].w0, 1) == sh.pending[1].n - 1;
       meet();
       __threadfence();
+      int turn = 0;
       for (int i = begun ? 0 : 1; i < (ended ? 2 : 1); ++i)
-        if (sh.last_one[i]) join_parts<D, BF16, Q>(p, sh.pending[i], ring_mem);
+        if (sh.last_one[i] && !join_parts(p, sh, sh.pending[i], ring_mem, turn)) break;
     }
   }
   // after a wait that gave up: no CTA leaves under a copy of its own
