@@ -11,30 +11,14 @@
 namespace lava {
 namespace {
 
-// Where row r of a head goes: behind one another in the packed cache,
-struct PackedRows {
-  long long row0;
-  __device__ __forceinline__ long long at(int r) const { return row0 + r; }
-};
-// or to the pages of a paged cache (-1: nowhere).
-struct PagedRows {
-  const int* pages;  // the head's row of the page table
-  int row0, shift, n_pages, max_rows;
-  __device__ __forceinline__ long long at(int r) const {
-    if (r >= max_rows - row0) return -1;
-    const int row = row0 + r, page = pages[row >> shift];
-    return (unsigned)page < (unsigned)n_pages ? ((long long)page << shift) + (row & ((1 << shift) - 1)) : -1;
-  }
-};
-
 // kAhead: rows a thread has on their way.  1 / 2 / 4 (20 and 32 registers for 1 and 2, in the cascade's kernel
 // 30 and 48): 32 layers x 8K 23.8 / 22.2 /
 // 25.4 us, 28 layers x 128K 20.3 / 20.4 / 23.2, ragged batch of 8 49.6 / 47.3 / 46.7 with eight blocks per
 // SM; where there is little to move one is better (see blocks_for).
-template <int kAhead, class Place>
+template <int kAhead>
 __device__ __forceinline__ void
 compact_head(const Geom& g, int prob, const char* k, const char* v, long long k_ls, long long v_ls,
-             const int* keep_idx, const int* head_offsets, const Place& place, char* k_out,
+             const int* keep_idx, const int* head_offsets, const long long* row_off, char* k_out,
              char* v_out, int blocks_per_head) {
   const int layer = prob / g.batch, b = prob - layer * g.batch;
   const int kvh = blockIdx.y;
@@ -49,6 +33,7 @@ compact_head(const Geom& g, int prob, const char* k, const char* v, long long k_
   const int kept = rows - win;  // kept prefix rows of this head
   // this head's kept positions: entries [h0 - kvh*win, ...) of the sequence's keep list
   const int* keep = keep_idx + (size_t)layer * g.total_scores + s.score_off + (h0 - kvh * win);
+  const long long out_row0 = row_off[prob] + h0;
   const char* kl = k + ((size_t)layer * k_ls + (long long)kvh * g.k_sh) * es;
   const char* vl = v + ((size_t)layer * v_ls + (long long)kvh * g.v_sh) * es;
 
@@ -72,19 +57,11 @@ compact_head(const Geom& g, int prob, const char* k, const char* v, long long k_
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
       if (r0 + u * step < rows) {
-        const long long row = place.at(r0 + u * step);
-        if (row < 0) continue;
-        const long long dst = row * row_bytes + c * 16;
+        const long long dst = (out_row0 + r0 + u * step) * row_bytes + c * 16;
         *reinterpret_cast<uint4*>(k_out + dst) = kk[u];
         *reinterpret_cast<uint4*>(v_out + dst) = vv[u];
       }
   }
-}
-
-// First row of the head that this block works on.
-__device__ __forceinline__ PackedRows packed_rows(const Geom& g, int prob, const int* head_offsets,
-                                                  const long long* row_off) {
-  return {row_off[prob] + head_offsets[(size_t)prob * (g.n_kv_heads + 1) + blockIdx.y]};
 }
 
 template <int kAhead>
@@ -94,25 +71,8 @@ compact_kernel(Geom g, const char* k, const char* v, long long k_ls, long long v
                char* k_out, char* v_out, int blocks_per_head) {
   in_stream_order();
   if (batch_has_short_sequence(g)) return;  // the score layout has no room for such a batch
-  compact_head<kAhead>(g, blockIdx.z, k, v, k_ls, v_ls, keep_idx, head_offsets,
-                       packed_rows(g, blockIdx.z, head_offsets, row_off), k_out, v_out, blocks_per_head);
-}
-
-// The same into pages: sequence b of the batch is first_seq + b of the cache.
-template <int kAhead>
-__global__ void __launch_bounds__(256)
-compact_pages_kernel(Geom g, Cache c, int first_seq, const char* k, const char* v, long long k_ls, long long v_ls,
-                     const int* keep_idx, const int* head_offsets, const int* first_row, const int* page_table,
-                     char* k_pages, char* v_pages, int blocks_per_head) {
-  in_stream_order();
-  if (batch_has_short_sequence(g)) return;  // the score layout has no room for such a batch
-  const int prob = blockIdx.z, layer = prob / g.batch, seq = first_seq + prob - layer * g.batch;
-  const int row0 = first_row[(size_t)prob * g.n_kv_heads + blockIdx.y];
-  if (row0 < 0) return;  // the head got no pages
-  const size_t head = ((size_t)layer * c.batch + seq) * c.n_kv_heads + blockIdx.y;
-  const PagedRows place = {page_table + head * c.max_pages, row0, c.page_shift, c.n_pages,
-                           c.max_pages << c.page_shift};
-  compact_head<kAhead>(g, prob, k, v, k_ls, v_ls, keep_idx, head_offsets, place, k_pages, v_pages, blocks_per_head);
+  compact_head<kAhead>(g, blockIdx.z, k, v, k_ls, v_ls, keep_idx, head_offsets, row_off, k_out, v_out,
+                       blocks_per_head);
 }
 
 // Rows of the lower layers move from the old arena to their place in the new one: for
@@ -175,8 +135,7 @@ cascade_rows_kernel(Geom g, int first, int n_lists, HeldLists io, const int* hof
                       k_new, v_new, blocks_per_head);
   else
     compact_head<kAhead>(g, z, k, v, 0, 0, keep_idx, hoff_new + (size_t)n_lists * (g.n_kv_heads + 1),
-                         packed_rows(g, z, hoff_new + (size_t)n_lists * (g.n_kv_heads + 1), io.row_off_new + n_lists),
-                         k_new, v_new, blocks_per_head);
+                         io.row_off_new + n_lists, k_new, v_new, blocks_per_head);
 }
 
 // Row counts live on the device, so the grid is sized for the bandwidth, not the data: enough
@@ -219,21 +178,6 @@ lava_status launch_compact(const Geom& g, int n_layers, const void* k, const voi
                                         v_ls, keep_idx, head_offsets, row_off, (char*)k_out, (char*)v_out, bph);
   count_launches(1);
   return check_cuda(e, "compact_kv launch");
-}
-
-lava_status launch_compact_pages(const Geom& g, const Cache& c, int first_seq, const void* k, const void* v,
-                                 long long k_ls, long long v_ls, const int* keep_idx, const int* head_offsets,
-                                 const int* first_row, const int* page_table, void* k_pages, void* v_pages,
-                                 cudaStream_t stream) {
-  const Blocks blocks = blocks_for(g, c.n_layers * g.batch);
-  const int bph = blocks.per_head;
-  dim3 grid(bph, g.n_kv_heads, c.n_layers * g.batch);
-  const auto kernel = blocks.two_ahead ? compact_pages_kernel<2> : compact_pages_kernel<1>;
-  const cudaError_t e = launch_in_order(kernel, grid, 256, 0, stream, g, c, first_seq, (const char*)k,
-                                        (const char*)v, k_ls, v_ls, keep_idx, head_offsets, first_row, page_table,
-                                        (char*)k_pages, (char*)v_pages, bph);
-  count_launches(1);
-  return check_cuda(e, "compact_kv_pages launch");
 }
 
 lava_status launch_cascade_rows(const Geom& g, int n_lists, const HeldLists& io, const int* hoff_new,

@@ -64,7 +64,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 1024;
+constexpr int kMostThreads = 1024;
 constexpr int kMostCtas = 8;
 
 struct TableParams {
@@ -121,40 +121,68 @@ struct Sums {
   int bad;
 };
 
-// Inclusive prefix sums over the block of two values; the totals in *sum.
-__device__ __forceinline__ longlong2 scan_block(int take, int give, longlong2* warps, longlong2* sum) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long a = take, b = give;
+// Inclusive prefix sums over the block; the totals in *sum.  (Sums that do not fit 32 bits belong to refused calls.)
+__device__ __forceinline__ int2 scan_block(int2 x, int2* warps, int2* sum) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
+  const auto scan = [&](int2 a) {
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long x = __shfl_up_sync(0xffffffffu, a, o), y = __shfl_up_sync(0xffffffffu, b, o);
-    if (lane >= o) {
-      a += x;
-      b += y;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, a.x, o), z = __shfl_up_sync(0xffffffffu, a.y, o);
+      if (lane >= o) a = make_int2(a.x + y, a.y + z);
     }
-  }
-  if (lane == 31) warps[warp] = make_longlong2(a, b);
+    return a;
+  };
+  x = scan(x);
+  if (lane == 31) warps[warp] = x;
   __syncthreads();
-  longlong2 before = make_longlong2(0, 0), all = make_longlong2(0, 0);
-  for (int w = 0; w < kThreads / 32; ++w) {
-    if (w == warp) before = all;
-    all.x += warps[w].x;
-    all.y += warps[w].y;
-  }
-  __syncthreads();
-  *sum = all;
-  return make_longlong2(a + before.x, b + before.y);
+  const int2 upto = scan(lane < n_warps ? warps[lane] : make_int2(0, 0));
+  *sum = make_int2(__shfl_sync(0xffffffffu, upto.x, 31), __shfl_sync(0xffffffffu, upto.y, 31));
+  const int y = __shfl_sync(0xffffffffu, upto.x, max(0, warp - 1)), z = __shfl_sync(0xffffffffu, upto.y, max(0, warp - 1));
+  __syncthreads();  // (the warps' sums are written again)
+  return warp ? make_int2(x.x + y, x.y + z) : x;
 }
 
-__global__ void __launch_bounds__(kThreads)
-page_table_kernel(const TableParams p) {
+// Entry i of the ring, counted from `start` (both below the ring's length).
+__device__ __forceinline__ int ring_at(int start, int i, int n) {
+  const int at = start + i;
+  return at < n ? at : at - n;
+}
+
+// Copies `n` numbers for every lane, from ring to table or back: lanes with up to two do it themselves, for the others
+// the warp does it, four lanes' at a time.
+template <class Copy>
+__device__ __forceinline__ void copy_pages(int n, const Copy& copy) {  // copy(lane whose numbers they are, which)
+  const int lane = threadIdx.x & 31;
+  if (n > 0 && n <= 2)
+    for (int i = 0; i < n; ++i) copy(lane, i);
+  unsigned many = __ballot_sync(0xffffffffu, n > 2);
+  while (many) {
+    int of[4], cnt[4], most = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      of[u] = many ? __ffs(many) - 1 : 0;
+      cnt[u] = __shfl_sync(0xffffffffu, n, of[u]);
+      if (!many) cnt[u] = 0;
+      many &= many - 1;
+      most = max(most, cnt[u]);
+    }
+    for (int i = lane; i < most; i += 32)
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (i < cnt[u]) copy(of[u], i);
+  }
+}
+
+__global__ void __launch_bounds__(kMostThreads)
+page_table_kernel(const __grid_constant__ TableParams p) {
   in_stream_order();
-  __shared__ longlong2 warps[kThreads / 32];
+  __shared__ int2 warps[32];
+  __shared__ long long take_sums[32], give_sums[32];
   __shared__ Sums mine;
-  __shared__ int ends[kThreads], held_at[kThreads];  // of the heads in hand: page numbers up to here, pages held
+  __shared__ int from[kMostThreads], to[kMostThreads];  // of a thread's head: where its pages start in ring and table
   const Cache& c = p.c;
   cg::cluster_group cluster = cg::this_cluster();
-  const int tid = threadIdx.x, ctas = gridDim.x, rank = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, ctas = gridDim.x, rank = blockIdx.x;
   const int share = (c.heads + ctas - 1) / ctas;
   const int h0 = min(c.heads, rank * share), h1 = min(c.heads, h0 + share);
   const long long taken = p.counters[0], given = p.counters[1];
@@ -162,8 +190,10 @@ page_table_kernel(const TableParams p) {
   // ---- what this CTA's heads need ---------------------------------------------------------------
   long long take = 0, give = 0;
   int bad = 0;
-  for (int h = h0 + tid; h < h1; h += kThreads) {
+  Change first = {};  // of this thread's first head
+  for (int h = h0 + tid; h < h1; h += threads) {
     const Change x = change_of(p, h);
+    if (h < h0 + threads) first = x;
     take += x.take;
     give += x.give;
     bad |= x.bad;
@@ -173,15 +203,20 @@ page_table_kernel(const TableParams p) {
     take += __shfl_xor_sync(0xffffffffu, take, o);
     give += __shfl_xor_sync(0xffffffffu, give, o);
   }
-  if ((tid & 31) == 0) warps[tid >> 5] = make_longlong2(take, give);
+  if (lane == 0) {
+    take_sums[warp] = take;
+    give_sums[warp] = give;
+  }
   bad = __syncthreads_or(bad);
-  if (tid == 0) {
-    Sums s = {0, 0, bad};
-    for (int w = 0; w < kThreads / 32; ++w) {
-      s.take += warps[w].x;
-      s.give += warps[w].y;
+  if (warp == 0) {
+    take = lane < threads / 32 ? take_sums[lane] : 0;
+    give = lane < threads / 32 ? give_sums[lane] : 0;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      take += __shfl_xor_sync(0xffffffffu, take, o);
+      give += __shfl_xor_sync(0xffffffffu, give, o);
     }
-    mine = s;
+    if (lane == 0) mine = {take, give, bad};
   }
   cluster.sync();
   long long take_at = 0, give_at = 0, take_all = 0, give_all = 0;
@@ -200,16 +235,21 @@ page_table_kernel(const TableParams p) {
   // (more pages given back than the pool has in use: the table and the counters do not belong together)
   if (!short_of && give_all > c.n_pages - (given - taken)) bad = 1;
   const bool refused = bad || short_of;
+  // where this CTA's pages start in the ring
+  int ring_take = refused ? 0 : (int)((taken + take_at) % c.n_pages), ring_give = refused ? 0 : (int)((given + give_at) % c.n_pages);
 
-  // ---- what they get: 1024 heads at a time --------------------------------------------------------
-  for (int at = h0; at < h1; at += kThreads) {
+  // ---- what they get, a head per thread at a time -------------------------------------------------
+  for (int at = h0; at < h1; at += threads) {
     const int h = at + tid;
     const bool live = h < h1;
-    Change x = {0, 0, 0, 0, 0, 0};
-    if (live) x = change_of(p, h);
-    longlong2 sum;
-    const longlong2 incl = scan_block(x.take, x.give, warps, &sum);
-    const long long first = taken + take_at + incl.x - x.take;  // in the ring
+    Change x = first;
+    if (at > h0) x = live ? change_of(p, h) : Change{};
+    if (!live) x = Change{};
+    if (refused) x.take = x.give = 0;
+    int2 sum;
+    const int2 incl = scan_block(make_int2(x.take, x.give), warps, &sum);
+    const int my_take = ring_at(ring_take, incl.x - x.take, c.n_pages);
+    const size_t row = (size_t)h * c.max_pages;
     if (live) {
       p.rows_out[h] = refused ? x.before : x.after;
       const int prob = h / c.n_kv_heads, g = h - prob * c.n_kv_heads, layer = prob / c.batch, b = prob - layer * c.batch;
@@ -220,46 +260,35 @@ page_table_kernel(const TableParams p) {
         for (int j = 0; j < p.max_add; ++j) {
           int slot = -1;
           if (j < n) {
-            const int row = x.before + j, pg = row >> c.page_shift;
-            const int page = pg < x.held ? p.table[(size_t)h * c.max_pages + pg]
-                                         : p.ring[(first + pg - x.held) % c.n_pages];
-            slot = page < 0 || page >= c.n_pages ? -1 : (page << c.page_shift) + (row & (c.page_rows - 1));
+            const int r = x.before + j, pg = r >> c.page_shift;
+            const int page = pg < x.held ? p.table[row + pg] : p.ring[ring_at(my_take, pg - x.held, c.n_pages)];
+            slot = page < 0 || page >= c.n_pages ? -1 : (page << c.page_shift) + (r & (c.page_rows - 1));
           }
           p.slots[((size_t)prob * p.max_add + j) * c.n_kv_heads + g] = slot;
         }
       }
     }
-    if (!refused && sum.x > 0) {  // new pages: a thread per page, whose head is found in the sums
-      ends[tid] = (int)incl.x;
-      held_at[tid] = x.held;
-      __syncthreads();
-      for (int e = tid; e < (int)sum.x; e += kThreads) {
-        int lo = 0, hi = kThreads - 1;  // the first head whose pages end behind e
-        while (lo < hi) {
-          const int mid = (lo + hi) >> 1;
-          if (ends[mid] > e) hi = mid; else lo = mid + 1;
-        }
-        const int in_head = e - (lo ? ends[lo - 1] : 0);
-        p.table[(size_t)(at + lo) * c.max_pages + held_at[lo] + in_head] = p.ring[(taken + take_at + e) % c.n_pages];
-      }
-      __syncthreads();
+    if (sum.x > 0) {  // new pages
+      from[tid] = my_take;
+      to[tid] = x.held;
+      __syncwarp();
+      copy_pages(x.take, [&](int l, int i) {
+        const int t = tid - lane + l;
+        p.table[(size_t)(at + t) * c.max_pages + to[t] + i] = p.ring[ring_at(from[t], i, c.n_pages)];
+      });
+      __syncwarp();
     }
-    if (!refused && sum.y > 0) {  // pages that go back
-      ends[tid] = (int)incl.y;
-      __syncthreads();
-      for (int e = tid; e < (int)sum.y; e += kThreads) {
-        int lo = 0, hi = kThreads - 1;
-        while (lo < hi) {
-          const int mid = (lo + hi) >> 1;
-          if (ends[mid] > e) hi = mid; else lo = mid + 1;
-        }
-        const int in_head = e - (lo ? ends[lo - 1] : 0);
-        p.ring_out[(given + give_at + e) % c.n_pages] = p.table[(size_t)(at + lo) * c.max_pages + in_head];
-      }
-      __syncthreads();
+    if (sum.y > 0) {  // pages that go back
+      from[tid] = ring_at(ring_give, incl.y - x.give, c.n_pages);
+      __syncwarp();
+      copy_pages(x.give, [&](int l, int i) {
+        const int t = tid - lane + l;
+        p.ring_out[ring_at(from[t], i, c.n_pages)] = p.table[(size_t)(at + t) * c.max_pages + i];
+      });
+      __syncwarp();
     }
-    take_at += sum.x;
-    give_at += sum.y;
+    ring_take = ring_at(ring_take, sum.x, c.n_pages);
+    ring_give = ring_at(ring_give, sum.y, c.n_pages);
   }
   cluster.sync();  // every CTA has read the counters and the others' sums
   if (rank == 0 && tid == 0) {
@@ -271,9 +300,10 @@ page_table_kernel(const TableParams p) {
 }
 
 lava_status launch_tables(const TableParams& p, cudaStream_t stream) {
-  // a CTA for every 1024 heads
+  // a CTA for every 128 heads and a thread per head, then more threads, then more heads per thread
   int ctas = 1;
-  while (ctas < kMostCtas && ctas * kThreads < p.c.heads) ctas *= 2;
+  while (ctas < kMostCtas && ctas * 128 < p.c.heads) ctas *= 2;
+  const int share = (p.c.heads + ctas - 1) / ctas, threads = std::min(kMostThreads, (share + 31) / 32 * 32);
   cudaLaunchAttribute attr[2] = {};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -282,7 +312,7 @@ lava_status launch_tables(const TableParams& p, cudaStream_t stream) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = ctas;
-  cfg.blockDim = kThreads;
+  cfg.blockDim = threads;
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
