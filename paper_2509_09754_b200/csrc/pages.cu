@@ -148,13 +148,17 @@ __device__ __forceinline__ int ring_at(int start, int i, int n) {
   return at < n ? at : at - n;
 }
 
-// Copies `n` numbers for every lane, from ring to table or back: lanes with up to two do it themselves, for the others
-// the warp does it, four lanes' at a time.
-template <class Copy>
-__device__ __forceinline__ void copy_pages(int n, const Copy& copy) {  // copy(lane whose numbers they are, which)
+// Moves `n` numbers for every lane, between ring and table: lanes with up to two do it themselves, for the others the
+// warp does it, four lanes' and two rounds at a time (all loads before the stores, which might be to the same memory for
+// all the compiler knows).
+template <class Load, class Store>
+__device__ __forceinline__ void move_pages(int n, const Load& load, const Store& store) {  // (whose lane's, which, value)
   const int lane = threadIdx.x & 31;
-  if (n > 0 && n <= 2)
-    for (int i = 0; i < n; ++i) copy(lane, i);
+  if (n > 0 && n <= 2) {
+    const int a = load(lane, 0), b = n == 2 ? load(lane, 1) : 0;
+    store(lane, 0, a);
+    if (n == 2) store(lane, 1, b);
+  }
   unsigned many = __ballot_sync(0xffffffffu, n > 2);
   while (many) {
     int of[4], cnt[4], most = 0;
@@ -166,10 +170,23 @@ __device__ __forceinline__ void copy_pages(int n, const Copy& copy) {  // copy(l
       many &= many - 1;
       most = max(most, cnt[u]);
     }
-    for (int i = lane; i < most; i += 32)
+    for (int i0 = 0; i0 < most; i0 += 64) {
+      int x[4][2];
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        if (i < cnt[u]) copy(of[u], i);
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const int i = i0 + 32 * v + lane;
+          x[u][v] = i < cnt[u] ? load(of[u], i) : 0;
+        }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const int i = i0 + 32 * v + lane;
+          if (i < cnt[u]) store(of[u], i, x[u][v]);
+        }
+    }
   }
 }
 
@@ -272,19 +289,17 @@ page_table_kernel(const __grid_constant__ TableParams p) {
       from[tid] = my_take;
       to[tid] = x.held;
       __syncwarp();
-      copy_pages(x.take, [&](int l, int i) {
-        const int t = tid - lane + l;
-        p.table[(size_t)(at + t) * c.max_pages + to[t] + i] = p.ring[ring_at(from[t], i, c.n_pages)];
-      });
+      const int t0 = tid - lane;
+      move_pages(x.take, [&](int l, int i) { return p.ring[ring_at(from[t0 + l], i, c.n_pages)]; },
+                 [&](int l, int i, int page) { p.table[(size_t)(at + t0 + l) * c.max_pages + to[t0 + l] + i] = page; });
       __syncwarp();
     }
     if (sum.y > 0) {  // pages that go back
       from[tid] = ring_at(ring_give, incl.y - x.give, c.n_pages);
       __syncwarp();
-      copy_pages(x.give, [&](int l, int i) {
-        const int t = tid - lane + l;
-        p.ring_out[ring_at(from[t], i, c.n_pages)] = p.table[(size_t)(at + t) * c.max_pages + i];
-      });
+      const int t0 = tid - lane;
+      move_pages(x.give, [&](int l, int i) { return p.table[(size_t)(at + t0 + l) * c.max_pages + i]; },
+                 [&](int l, int i, int page) { p.ring_out[ring_at(from[t0 + l], i, c.n_pages)] = page; });
       __syncwarp();
     }
     ring_take = ring_at(ring_take, sum.x, c.n_pages);
