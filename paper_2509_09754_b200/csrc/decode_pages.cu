@@ -488,7 +488,9 @@ struct Plan {
 
 // Heads that are short against a warp's share go whole to warps, which then need not meet.  Else, where few CTAs have
 // work, a portion is cut into pieces of 128 or 256 KB, no more than there are CTAs; and where there is more, the line
-// into equal parts.
+// into equal parts.  (SMs do not get equal shares of the bandwidth: of 64 x 8 heads of 2048 rows the first CTA is through
+// after 68 us, the last after 86.  An eighth of the line in small parts for whoever is through did not pay: 105 us against
+// 96, with a twelfth in fewer parts 101; every small part has its own meeting, partial results and joins.)
 template <class S>
 __device__ __forceinline__ Plan plan_of(const PageParams& p, const Counts& all) {
   Plan plan = {0, 0, 0, all.tiles * p.subs};
@@ -533,6 +535,7 @@ struct Pending {
 template <int D, bool BF16, int Q>
 using WarpOf = typename std::conditional<BF16, TensorWarp<D, Q>, PlainWarp<D, Q>>::type;
 
+constexpr int kFew = 8;     // CTAs whose results are joined straight from memory, at most
 constexpr int kSegs = 64;  // segments of heads that are counted, at most
 
 template <int D, bool BF16, int Q>
@@ -784,6 +787,37 @@ __device__ __forceinline__ bool join_parts(const PageParams& p, Shared<D, BF16, 
   }
   if (tid == 0) p.counters[x.w0] = 0;  // ready for the next call
   return true;
+}
+
+// The same for few CTAs, straight from memory: a thread has four columns of a query and loads them of all CTAs at once.
+template <int D, bool BF16, int Q>
+__device__ __forceinline__ void join_few(const PageParams& p, const Pending& x) {
+  const int n = x.n;
+  const auto slot = [&](int i) { return (size_t)(x.w0 + i) * 2 + (i == 0); };
+  for (int e = threadIdx.x; e < x.queries * (D / 4); e += kConsumers * 32) {
+    const int q = e / (D / 4), col = e % (D / 4) * 4;
+    float2 ml[kFew];
+    float4 f[kFew];
+#pragma unroll
+    for (int i = 0; i < kFew; ++i) {
+      ml[i] = i < n ? __ldcg(p.part_ml + slot(i) * Q + q) : make_float2(-INFINITY, 0.f);
+      f[i] = i < n ? __ldcg(reinterpret_cast<const float4*>(p.part + (slot(i) * Q + q) * D + col)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    float top = ml[0].x;
+#pragma unroll
+    for (int i = 1; i < kFew; ++i) top = fmaxf(top, ml[i].x);
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+#pragma unroll
+    for (int i = 0; i < kFew; ++i) {
+      const float w = fast_exp2(ml[i].x - finite_ref(top));
+      a = make_float4(fmaf(w, f[i].x, a.x), fmaf(w, f[i].y, a.y), fmaf(w, f[i].z, a.z), fmaf(w, f[i].w, a.w));
+      l = fmaf(w, ml[i].y, l);
+    }
+    store4<BF16>(p.out, (x.q_row + q) * D + col, make_float4(a.x / l, a.y / l, a.z / l, a.w / l));
+    if (p.lse && col == 0) p.lse[x.q_row + q] = (top + fast_log2(l)) * kLn2;
+  }
+  if (threadIdx.x == 0) p.counters[x.w0] = 0;  // ready for the next call
 }
 
 template <int D, bool BF16, int Q>
@@ -1046,7 +1080,11 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
       __threadfence();
       int turn = 0;
       for (int i = begun ? 0 : 1; i < (ended ? 2 : 1); ++i)
-        if (sh.last_one[i] && !join_parts(p, sh, sh.pending[i], ring_mem, turn)) break;
+        if (sh.last_one[i]) {
+          const Pending x = sh.pending[i];
+          if (x.n <= kFew) join_few<D, BF16, Q>(p, x);
+          else if (!join_parts(p, sh, x, ring_mem, turn)) break;
+        }
     }
   }
   // after a wait that gave up: no CTA leaves under a copy of its own
