@@ -42,9 +42,10 @@ def parse_args():
     ap.add_argument("--e2e-steps", type=int, default=5)
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-e2e", action="store_true")
-    ap.add_argument("--path", default="evict", choices=["evict", "cascade", "decode"],
+    ap.add_argument("--path", default="evict", choices=["evict", "cascade", "decode", "paged"],
                     help="evict: the one-shot hot path (the headline line); cascade: Algorithm 2 one "
-                         "layer per call; decode: attention of one new token over the packed cache")
+                         "layer per call; decode: attention of one new token over the packed cache; "
+                         "paged: a decode step over the paged cache, layer by layer")
     ap.add_argument("--layers", type=int, default=0,
                     help="run only the first N layers of the workload (small cases for profiling; "
                          "the budget shrinks in proportion and the line says so)")
@@ -269,8 +270,8 @@ def run_reference(args, rank):
 
 # ----------------------------------------------------------------------------- further paths
 def run_next_path(args, cfg, plan, q, k, v, stream, steps, warmup, local_rank, rank, world):
-    """The layer-by-layer cascade (Algorithm 2) or the decode-time consumer of the packed cache,
-    timed like the headline path (CUDA events, clocks sampled, one JSON line)."""
+    """The layer-by-layer cascade (Algorithm 2), the decode-time consumer of the packed cache or a decode
+    step over the paged cache, timed like the headline path (CUDA events, clocks sampled, one JSON line)."""
     import torch
     import paper_2509_09754_b200 as lava
     from paper_2509_09754_b200 import replicas
@@ -292,6 +293,37 @@ def run_next_path(args, cfg, plan, q, k, v, stream, steps, warmup, local_rank, r
         note = ("K + V read once + the final packed cache; every step also re-evicts all lower "
                 "layers (rows moved once per step), which this figure does not credit")
         workspace = cas.workspace
+    elif args.path == "paged":
+        B, H, Hq, ps, dev = cfg.batch, cfg.n_kv_heads, cfg.n_q_heads, 64, q.device
+        grown = steps + warmup
+        code = lava.LAVA_BF16 if cfg.dtype == "bf16" else lava.LAVA_F32
+        cache = lava.PagedCache(lava.CacheDesc(
+            n_layers=L, batch=B, n_q_heads=Hq, n_kv_heads=H, head_dim=d, dtype=code, page_rows=ps,
+            max_pages=-(-(max(cfg.seq_lens) + grown) // ps),
+            n_pages=rows // ps + L * B * H * (2 + grown // ps)), device=dev)
+        cache.admit(plan, k, v)
+        gen = torch.Generator(device="cpu").manual_seed(3)
+        qkv = torch.randn((B, (Hq + 2 * H) * d), generator=gen).to(q.dtype).to(dev)
+        q_new, k_new, v_new = (qkv[:, i * d: j * d].view(B, j - i, d)
+                               for i, j in ((0, Hq), (Hq, Hq + H), (Hq + H, Hq + 2 * H)))
+        freqs = lava.lava_rotary_freqs(d, 500000.0)[0].to(dev)
+        rotary = lava.RotaryDesc(head_dim=d, rotary_dim=d, dtype=code)
+        add = torch.ones(B, dtype=torch.int32, device=dev)
+        pos = torch.tensor(cfg.seq_lens, dtype=torch.int32, device=dev)
+        turned = torch.empty((B, Hq, d), dtype=q.dtype, device=dev)
+        out = torch.empty_like(turned)
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=dev)
+
+        def step():
+            cache.extend(add, stream=stream)
+            for l in range(L):
+                cache.append(rotary, freqs, l, pos, q_new, k_new, v_new, turned, stream)
+                cache.attend(l, turned, out, lse, stream)
+        metric, unit, units = "cached KV rows/s read by one paged decode step, layer by layer", "rows/s", rows
+        alg_bytes = rows * 2 * d * es
+        note = ("one K row and one V row per retained (KV head, position); a step extends the tables once and, in "
+                "every layer, appends the new token's rows and attends")
+        workspace = cache.workspace
     else:
         dev = q.device
         gen = torch.Generator(device="cpu").manual_seed(3)

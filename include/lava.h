@@ -393,7 +393,8 @@ typedef struct lava_cache_desc {
   int32_t head_dim;    /* 64 or 128                                                         */
   int32_t dtype;       /* lava_dtype of the pages, the queries and the attention's output   */
   int32_t page_rows;   /* 16, 32, 64, 128 or 256                                            */
-  int32_t max_pages;   /* pages of a head at most = row length of page_table                */
+  int32_t max_pages;   /* pages of a head at most = row length of page_table;
+                          max_pages * page_rows < 2^30                                      */
   int64_t n_pages;     /* pages of the pool; n_pages * page_rows < 2^31                     */
   float sm_scale;      /* logit scale; 0 => 1/sqrt(head_dim)                                */
   float softcap;       /* 0 => none; else a logit x becomes softcap * tanh(x / softcap)     */

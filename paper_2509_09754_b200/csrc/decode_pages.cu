@@ -67,6 +67,7 @@ struct PageParams {
   int* counters;           // [CTA]: CTAs that have left their result of the portion that begins last in this one's part
   unsigned* status;
   long long wait_cycles;
+  int sleep;               // waits sleep between two looks (0 where the limit is shorter than that)
 };
 
 struct Ctl {
@@ -692,7 +693,8 @@ __device__ __forceinline__ void whole_heads(const PageParams& p, const CUtensorM
       fetched = min(q_row + p.c.group, p.queries - p.c.group);
       w.fetch(p, fetched, p.c.group);
     }
-    alive = __all_sync(0xffffffffu, wait_bar(smem_u32(&sh.full_own[stage][warp]), (i / S::kStages) & 1, &sh.ctl, p.status));
+    alive = __all_sync(0xffffffffu, wait_bar(smem_u32(&sh.full_own[stage][warp]), (i / S::kStages) & 1, &sh.ctl, p.status,
+                                             true, p.sleep));
     if (!alive) break;
     const uint32_t k_tile = ring + stage * S::kStageBytes;
     w.tile(k_tile, k_tile + S::kTileBytes, warp * kBoxRows, min(kBoxRows, len - row), logit, q_mem,
@@ -943,7 +945,7 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     }
   }
   const auto wait = [&](uint64_t* bar, int parity) {  // the same in all lanes
-    return __all_sync(0xffffffffu, wait_bar(smem_u32(bar), parity, &sh.ctl, p.status)) != 0;
+    return __all_sync(0xffffffffu, wait_bar(smem_u32(bar), parity, &sh.ctl, p.status, true, p.sleep)) != 0;
   };
   int stage = 0, parity = 0;
   const auto next_stage = [&] {
@@ -1183,6 +1185,7 @@ lava_status lava_decode_attention_pages(const lava_cache_desc* cache, int32_t fi
   p.part = (float*)(ws + kStatusBytes + counter_bytes());
   p.part_ml = (float2*)((char*)p.part + up256(slots_of(c) * c.head_dim * sizeof(float)));
   p.wait_cycles = options().wait_limit_cycles;
+  p.sleep = p.wait_cycles >= 4000;
   cudaStream_t st = (cudaStream_t)stream;
   if (c.dtype == LAVA_BF16) {
     if (c.head_dim == 128)

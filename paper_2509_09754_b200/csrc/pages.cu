@@ -33,8 +33,8 @@ lava_status make_cache(const lava_cache_desc* d, Cache* out) {
     return fail(LAVA_ERR_UNSUPPORTED, "page_rows must be 16, 32, 64, 128 or 256 (got %d)", d->page_rows);
   if (d->max_pages < 1 || d->n_pages < 1)
     return fail(LAVA_ERR_INVALID_ARG, "max_pages and n_pages must be >= 1");
-  if (d->n_pages > 0x7fffffffLL / d->page_rows || d->max_pages > 0x7fffffff / d->page_rows)
-    return fail(LAVA_ERR_UNSUPPORTED, "rows of the pool and of a head must fit in 31 bits");
+  if (d->n_pages > 0x7fffffffLL / d->page_rows || d->max_pages > 0x3fffffff / d->page_rows)
+    return fail(LAVA_ERR_UNSUPPORTED, "rows of the pool must stay below 2^31, those of a head below 2^30");
   const long long heads = (long long)d->n_layers * d->batch * d->n_kv_heads;
   if ((long long)d->n_layers * d->batch > (1 << 24) || heads > (1 << 24))
     return fail(LAVA_ERR_UNSUPPORTED, "more than 2^24 heads");

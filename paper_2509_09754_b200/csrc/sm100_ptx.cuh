@@ -54,6 +54,17 @@ __device__ inline bool mbar_try(uint32_t bar, uint32_t parity, uint32_t ns) {
       : "memory");
   return ok != 0;
 }
+// The same look without sleeping (the blocking form may sleep longer than it is asked to).
+__device__ inline bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      "selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 __device__ inline uint64_t policy_evict_first() {
   uint64_t p;
   asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
@@ -282,11 +293,11 @@ __device__ inline void give_up(Ctl* m, unsigned* status) {
 // the drain waits at exit must outlast an abort to let copies in flight land).
 template <class Ctl>
 __device__ inline bool wait_bar(uint32_t bar, uint32_t parity, Ctl* m, unsigned* status,
-                                bool heed_abort = true) {
-  if (mbar_try(bar, parity, 1000)) return true;
+                                bool heed_abort = true, bool sleep = true) {
+  if (sleep ? mbar_try(bar, parity, 1000) : mbar_test(bar, parity)) return true;
   const long long t0 = clock64();
   for (;;) {
-    if (mbar_try(bar, parity, 1000)) return true;
+    if (sleep ? mbar_try(bar, parity, 1000) : mbar_test(bar, parity)) return true;
     if (heed_abort && m->abort_flag) return false;
     if (clock64() - t0 > (heed_abort ? m->wait_cycles : kWaitCycles)) break;
   }

@@ -138,6 +138,73 @@ def test_more_heads_than_a_block_has_threads():
     _check(rows.tolist(), group=1, d=64, page_rows=16)
 
 
+@pytest.mark.parametrize("dtype,d,group", [(torch.bfloat16, 128, 4), (torch.bfloat16, 128, 8), (torch.bfloat16, 128, 12),
+                                           (torch.bfloat16, 64, 16), (torch.bfloat16, 64, 20), (torch.float32, 64, 2),
+                                           (torch.float32, 64, 8), (torch.float32, 64, 9), (torch.float32, 128, 3)])
+def test_many_short_heads(dtype, d, group):
+    """Thousands of heads of a few boxes of 16 rows, some without rows: whole heads per warp where the type allows it."""
+    g = np.random.default_rng(d + group)
+    rows = np.where(g.random((5, 90, 8)) < 0.2, 0, g.integers(1, 50, (5, 90, 8)))
+    rows[0, 0], rows[4, 89] = 0, 0                                   # at both ends too
+    rows[2, 45, 3] = 64
+    _check(rows.tolist(), group=group, d=d, dtype=dtype, page_rows=16)
+
+
+@pytest.mark.parametrize("rows,group", [([[[9000, 100]]], 20), ([[[3000, 1700, 0, 2500]]] * 5, 40), ([[[2600] * 8]] * 9, 2)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_long_heads_and_large_groups(rows, group, dtype):
+    """Pieces of both sizes and equal parts of the line, one and several portions of a group's queries."""
+    _check(rows, group=group, d=64, dtype=dtype)
+
+
+def test_first_rows_at_minus_infinity_over_many_tiles():
+    """-inf logits fill whole tiles, pieces and parts before the first finite one."""
+    c = Case([[[3000, 40]]], group=2, dtype=torch.float32, d=64)
+    c.q.copy_(c.q.abs() + 0.1)
+    table = c.table[0, 0, 0].cpu()
+    c.k.view(-1, 64)[[int(table[j // 64]) * 64 + j % 64 for j in range(2900)]] = -float("inf")
+    out, lse = c.run()
+    k, v = c.flat[0]
+    c.flat[0] = (k[2900:], v[2900:])
+    c.check(out, lse)
+
+
+@pytest.mark.parametrize("L,rows", [(1, 2048), (32, 64)])
+def test_an_expired_wait_is_reported_and_a_zeroed_workspace_serves_again(L, rows):
+    """With a limit of one cycle a wait gives up at its second look: those for the first rows do (512 long heads by all
+    warps, 16384 short ones by a warp each).  The kernel returns, and the status word says so."""
+    B, H, d, ps = 64, 8, 128, 64
+    held = rows // ps
+    cache = lava.CacheDesc(n_layers=L, batch=B, n_q_heads=4 * H, n_kv_heads=H, head_dim=d, page_rows=ps, max_pages=held,
+                           n_pages=L * B * H * held)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, v = (torch.randn((cache.n_pages, ps, d), generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    table = torch.randperm(cache.n_pages, generator=g, device="cuda").int().view(L, B, H, held)
+    counts = torch.full((L, B, H), rows, dtype=torch.int32, device="cuda")
+    q = torch.randn((L, B, 4 * H, d), generator=g, device="cuda", dtype=torch.bfloat16)
+    ws = torch.zeros(lava.lava_cache_workspace_bytes(cache), dtype=torch.uint8, device="cuda")
+
+    def run():
+        out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device="cuda")
+        lava.lava_decode_attention_pages(cache, 0, q, k, v, table, counts, out, lse, ws)
+        return out, lse
+
+    want = run()
+    normal = lava.lava_get_option("wait_limit_cycles")
+    try:
+        lava.lava_set_option("wait_limit_cycles", 1)
+        run()
+        with pytest.raises(lava.LavaError) as err:
+            lava.lava_poll_status(ws)
+        assert err.value.status == 5                                   # LAVA_ERR_TIMEOUT
+    finally:
+        lava.lava_set_option("wait_limit_cycles", normal)
+    ws.zero_()
+    got = run()
+    assert lava.lava_poll_status(ws) == 0
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_a_cache_without_any_rows():
     _, out, lse = _check([[[0, 0], [0, 0]]], behind=1.0)
     assert bool((out == 0).all()) and bool((lse == -math.inf).all())
