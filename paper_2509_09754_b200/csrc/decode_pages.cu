@@ -20,6 +20,7 @@
 // queries per KV head than 16 are taken 16 at a time.  fp32: a lane has a row (or a half or quarter of it) for the
 // logits, and some columns for the product with V; up to 8 queries at a time.
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include <math.h>
@@ -54,7 +55,7 @@ struct Shape {
 struct PageParams {
   Cache c;
   int first_head;          // of the call's first layer
-  int heads, queries;      // of the call's layers
+  int heads;               // of the call's layers
   int subs, per_sub;       // a group's queries are taken in `subs` portions of `per_sub`
   int own_queries;         // a warp can have a head of its own
   const void* q;           // [layers, batch, H_q, d]
@@ -562,11 +563,8 @@ __device__ __forceinline__ int place(const PageParams& p, int h, int row) {
   return (unsigned)page < (unsigned)c.n_pages ? (page << c.page_shift) + (row & (c.page_rows - 1))
                                               : c.n_pages << c.page_shift;
 }
-// First row of the outputs, and of the queries, of a head's first query.
-__device__ __forceinline__ size_t first_query(const Cache& c, int h) {
-  const int prob = h / c.n_kv_heads, kvh = h - prob * c.n_kv_heads;
-  return (size_t)prob * c.n_q_heads + (size_t)kvh * c.group;
-}
+// First row of the queries, and of the outputs, of a KV head: query heads lie in the order of their KV heads.
+__device__ __forceinline__ size_t first_query(const Cache& c, int h) { return (size_t)h * c.group; }
 // Inclusive prefix sum over the warp.
 __device__ __forceinline__ int scan_warp(int x) {
   const int lane = threadIdx.x & 31;
@@ -620,11 +618,11 @@ __device__ __forceinline__ void whole_heads(const PageParams& p, const CUtensorM
   WarpOf<D, BF16, Q> w;
   const Logit logit(p.c);
   struct Batch {
-    int head, row, len, at, q_row;  // this lane's box
+    int head, row, len, at;  // this lane's box
   };
   int next_head = h, next_row = 0;  // the first box that is not in a batch yet
   const auto look_up = [&] {
-    Batch b = {end, 0, 0, 0, 0};
+    Batch b = {end, 0, 0, 0};
     int n = 0;  // boxes in the batch
     while (n < 32 && next_head < end) {
       // boxes of the next 32 heads, counted on from those in hand
@@ -655,10 +653,7 @@ __device__ __forceinline__ void whole_heads(const PageParams& p, const CUtensorM
       }
       n += took;
     }
-    if (lane < n) {
-      b.at = place(p, b.head, b.row);
-      b.q_row = (int)first_query(p.c, b.head);
-    }
+    if (lane < n) b.at = place(p, b.head, b.row);
     return b;
   };
   Batch cur = look_up(), nxt = look_up();
@@ -684,14 +679,12 @@ __device__ __forceinline__ void whole_heads(const PageParams& p, const CUtensorM
     }
     const int head = __shfl_sync(0xffffffffu, cur.head, i - first), row = __shfl_sync(0xffffffffu, cur.row, i - first);
     const int len = __shfl_sync(0xffffffffu, cur.len, i - first), stage = i % S::kStages;
-    const int q_row = __shfl_sync(0xffffffffu, cur.q_row, i - first);
     if (head != in_hand) {
-      if (fetched != q_row) w.fetch(p, q_row, p.c.group);
+      if (fetched != head) w.fetch(p, first_query(p.c, head), p.c.group);
       w.begin(q_mem);
       in_hand = head;
-      // the next head's, in case it follows (queries of neighbouring heads are neighbours)
-      fetched = min(q_row + p.c.group, p.queries - p.c.group);
-      w.fetch(p, fetched, p.c.group);
+      fetched = min(head + 1, p.heads - 1);  // the next head's, in case it follows
+      w.fetch(p, first_query(p.c, fetched), p.c.group);
     }
     alive = __all_sync(0xffffffffu, wait_bar(smem_u32(&sh.full_own[stage][warp]), (i / S::kStages) & 1, &sh.ctl, p.status,
                                              true, p.sleep));
@@ -701,7 +694,7 @@ __device__ __forceinline__ void whole_heads(const PageParams& p, const CUtensorM
            sh.probs[BF16 ? 0 : warp]);
     __syncwarp();
     if (sent < boxes) send();
-    if (row + kBoxRows >= len) w.finish(p, q_row, p.c.group);
+    if (row + kBoxRows >= len) w.finish(p, first_query(p.c, head), p.c.group);
   }
   if (!alive && lane == 0)  // no warp leaves under a copy of its own
     for (int i = max(0, sent - S::kStages); i < sent; ++i)
@@ -960,7 +953,7 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     // ---- producer ----------------------------------------------------------------------------------
     constexpr int kBoxes = S::kTile / kBoxRows, kAhead = 32 / kBoxes;
     bool alive = true;
-    for (; done < part.tiles && alive; ++h, sub = 0) {
+    for (; done < part.tiles && alive && h < p.heads; ++h, sub = 0) {
       const int len = head_len(p, h), n = tiles_of<S>(len);
       if (n == 0) continue;
       for (; sub < p.subs && done < part.tiles && alive; ++sub, t0 = 0) {
@@ -998,7 +991,7 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     float* const probs = sh.probs[BF16 ? 0 : warp];
     int fetched = -1;  // the head whose queries are on their way
     bool alive = true, begun = false, ended = false;  // others have tiles of the portion that the part begins, ends in
-    for (; done < part.tiles && alive; ++h, sub = 0) {
+    for (; done < part.tiles && alive && h < p.heads; ++h, sub = 0) {
       const int len = head_len(p, h), n = tiles_of<S>(len);
       if (n == 0) continue;
       for (; sub < p.subs && done < part.tiles; ++sub, t0 = 0) {
@@ -1118,9 +1111,16 @@ template <int D, bool BF16, int Q>
 lava_status launch(const CUtensorMap& map_k, const CUtensorMap& map_v, PageParams& p, cudaStream_t stream) {
   using S = Shape<D, BF16, Q>;
   const auto kernel = decode_pages_kernel<D, BF16, Q>;
-  const lava_status rc = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem),
-                                    "paged decode attention attribute");
+  static std::atomic<unsigned long long> told{0};  // devices that know how much shared memory the kernel takes
+  int dev = 0;
+  lava_status rc = check_cuda(cudaGetDevice(&dev), "current device");
   if (rc != LAVA_OK) return rc;
+  if (dev >= 64 || !(told.load(std::memory_order_relaxed) >> dev & 1)) {
+    rc = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem),
+                    "paged decode attention attribute");
+    if (rc != LAVA_OK) return rc;
+    if (dev < 64) told.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
   const long long most = ((((long long)p.c.max_pages << p.c.page_shift) + S::kTile - 1) / S::kTile) * p.heads * p.subs;
   const int grid = (int)std::min<long long>(most_ctas(), most);
   p.own_queries = WarpOf<D, BF16, Q>::kOwnQueries;
@@ -1171,7 +1171,6 @@ lava_status lava_decode_attention_pages(const lava_cache_desc* cache, int32_t fi
   if (rc != LAVA_OK) return rc;
   p.first_head = first_layer * c.batch * c.n_kv_heads;
   p.heads = n_layers * c.batch * c.n_kv_heads;
-  p.queries = p.heads * c.group;
   p.subs = portions.subs;
   p.per_sub = portions.per_sub;
   p.q = q;
