@@ -6,10 +6,11 @@
 // head's group share the read of its rows.  What has to be read is the rows, once; everything else is small, so the
 // kernel is built to keep copies in flight:
 //
-// The tiles of all heads (64 rows; 32 of 512 bytes) form one line, which is cut into equal parts, one per CTA, two
-// CTAs per SM: heads of any lengths load all SMs alike.  Row counts live on the device, so every CTA finds its part
-// itself.  A producer warp walks the part: it looks up the tile's pages and has TMA fetch K and V in boxes of 16 rows
-// (the least page) into a ring of stages; boxes behind a head's last row are not fetched.  Four warps consume a
+// The rows of all heads, in boxes of 16, form one line, which is cut into equal parts, one per CTA, two CTAs per SM: heads
+// of any lengths load all SMs alike.  Rows are worked on in tiles (64 rows of a head; 32 of 512 bytes), and a tile is in
+// the part that its first box is in.  Row counts live on the device, so every CTA finds its part
+// itself.  A producer warp walks the part: it looks up the tile's pages and has TMA fetch K and V in boxes (16 rows are
+// the least page) into a ring of stages; boxes behind a head's last row are not fetched.  Four warps consume a
 // tile, a quarter of its rows each, with maxima and sums of their own until the head or the part ends; then they meet
 // through the memory of the last stage.  A head inside one part is finished there.  Of a head that continues in other
 // parts the partial result goes to memory; the CTA that comes last, as a counter tells, joins them in order.
@@ -82,25 +83,20 @@ __device__ __forceinline__ int tiles_of(int len) {
 }
 // Sums over heads (the host has seen to it that they fit).
 struct Counts {
-  int tiles, boxes, small, large;  // tiles, boxes of 16 rows, pieces of both sizes
-  int most, empty;                 // boxes of the longest head; heads without rows
+  int boxes, small, large;  // boxes of 16 rows, pieces of both sizes
   template <class S>
   static __device__ __forceinline__ Counts of(int len) {
-    const int tiles = tiles_of<S>(len), boxes = (len + kBoxRows - 1) / kBoxRows;
-    return {tiles, boxes, (tiles + S::kSmall - 1) / S::kSmall, (tiles + S::kLarge - 1) / S::kLarge, boxes, len == 0};
+    const int tiles = tiles_of<S>(len);
+    return {(len + kBoxRows - 1) / kBoxRows, (tiles + S::kSmall - 1) / S::kSmall, (tiles + S::kLarge - 1) / S::kLarge};
   }
   __device__ __forceinline__ void add(const Counts& y) {
-    tiles += y.tiles;
     boxes += y.boxes;
     small += y.small;
     large += y.large;
-    most = max(most, y.most);
-    empty += y.empty;
   }
   __device__ __forceinline__ Counts over_warp() const {
-    return {__reduce_add_sync(0xffffffffu, tiles), __reduce_add_sync(0xffffffffu, boxes),
-            __reduce_add_sync(0xffffffffu, small), __reduce_add_sync(0xffffffffu, large),
-            __reduce_max_sync(0xffffffffu, most), __reduce_add_sync(0xffffffffu, empty)};
+    return {__reduce_add_sync(0xffffffffu, boxes), __reduce_add_sync(0xffffffffu, small),
+            __reduce_add_sync(0xffffffffu, large)};
   }
 };
 __device__ __forceinline__ int head_len(const PageParams& p, int h) {
@@ -480,12 +476,16 @@ __device__ __forceinline__ void store4(void* out, size_t at, float4 x) {  // `at
     *reinterpret_cast<float4*>(reinterpret_cast<float*>(out) + at) = x;
 }
 
-// How the line of tiles is cut (the same in every CTA: it follows from the row counts).
+template <class S>
+constexpr int kBoxesOf = S::kTile / kBoxRows;  // boxes of a tile
+constexpr int kPieceHeads = 1024;              // heads above which pieces are not counted
+
+// How the line is cut (the same in every CTA: it follows from the row counts).
 struct Plan {
   int by_warp;  // 1: whole heads per warp
   int piece;    // > 0: a portion's tiles in pieces of at most so many, one per CTA
   int parts;    // CTAs that have a part
-  int total;    // tiles of all portions (the host has seen to it that 32 bits hold them)
+  int total;    // boxes of all portions (the host has seen to it that 32 bits hold them)
 };
 
 // Heads that are short against a warp's share go whole to warps, which then need not meet.  Else, where few CTAs have
@@ -494,20 +494,21 @@ struct Plan {
 // after 68 us, the last after 86.  An eighth of the line in small parts for whoever is through did not pay: 105 us against
 // 96, with a twelfth in fewer parts 101; every small part has its own meeting, partial results and joins.)
 template <class S>
-__device__ __forceinline__ Plan plan_of(const PageParams& p, const Counts& all) {
-  Plan plan = {0, 0, 0, all.tiles * p.subs};
+__device__ __forceinline__ Plan plan_of(const PageParams& p, const Counts& all, int most) {  // most: boxes of the longest head
+  Plan plan = {0, 0, 0, all.boxes * p.subs};
   const int grid = gridDim.x;
-  if (S::kWarpRows == kBoxRows && p.subs == 1 && p.own_queries && (long long)all.most * grid * kConsumers <= 2ll * all.boxes) {
+  if (S::kWarpRows == kBoxRows && p.subs == 1 && p.own_queries && (long long)most * grid * kConsumers <= 2ll * all.boxes) {
     plan.by_warp = 1;
     plan.parts = grid;
-  } else if (all.small * p.subs <= grid) {
+  } else if (p.heads <= kPieceHeads && all.small * p.subs <= grid) {
     plan.piece = S::kSmall;
     plan.parts = all.small * p.subs;
-  } else if (all.large * p.subs <= grid) {
+  } else if (p.heads <= kPieceHeads && all.large * p.subs <= grid) {
     plan.piece = S::kLarge;
     plan.parts = all.large * p.subs;
   } else {
-    plan.parts = min(grid, plan.total);
+    // (a part is as long as a tile at least, so that a tile begins in it)
+    plan.parts = min(grid, max(min(plan.total, 1), plan.total / kBoxesOf<S>));
   }
   return plan;
 }
@@ -521,10 +522,10 @@ __device__ __forceinline__ int part_of(int total, int parts, int u) {
   return u < longer * (size + 1) ? u / (size + 1) : longer + (u - longer * (size + 1)) / size;
 }
 
-// A CTA's part: its first tile, and how many it has.
+// A CTA's part: its first tile, and where it ends.
 struct Part {
   int head, sub, tile;   // head of the call, portion of its queries, tile in it
-  int tiles;
+  int at, end;           // the line's box that the portion begins with, and the first one behind the part
   int first, pieces;     // of a piece: the portion's first piece and their number
 };
 
@@ -550,6 +551,7 @@ struct Shared {
   int issued, last_one[2];
   Pending pending[2];                                  // the portions that the part begins and ends in
   Counts segs[kSegs];
+  int2 seen[kThreads / 32];                            // by warp: boxes of the longest head, heads without rows
   float2 stats[kConsumers][Q];
   alignas(16) unsigned char q_mem[Warp::kOwnQueries ? kConsumers : 1][Warp::kQueryBytes];
   alignas(16) float probs[BF16 ? 1 : kConsumers][BF16 ? 4 : S::kWarpRows * Q];
@@ -848,16 +850,23 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   // ---- the cut: segments of heads are counted, a warp each; every warp finds what it needs ----------
   int seg_heads = 32;  // a power of two
   while (seg_heads * kSegs < p.heads) seg_heads *= 2;
-  if (p.heads <= 32 * kWarpsAll) {  // (little code: it is fetched anew by every launch)
-    const int h = 32 * warp + lane;
-    if (32 * warp < p.heads) {
-      const Counts sum = (h < p.heads ? Counts::of<S>(head_len(p, h)) : Counts{}).over_warp();
-      if (lane == 0) sh.segs[warp] = sum;
+  // (Little code for few heads: it is fetched anew by every launch.)
+  int most = 0, empty = 0;  // boxes of the longest head, heads without rows
+  const auto see = [&](int len) {
+    most = max(most, (len + kBoxRows - 1) / kBoxRows);
+    empty += len == 0;
+    return Counts::of<S>(len);
+  };
+  if (p.heads <= kPieceHeads) {
+    for (int seg = warp; 32 * seg < p.heads; seg += kWarpsAll) {
+      const int h = 32 * seg + lane;
+      const Counts sum = (h < p.heads ? see(head_len(p, h)) : Counts{}).over_warp();
+      if (lane == 0) sh.segs[seg] = sum;
     }
   } else {
     const int span = max(512, seg_heads), per_seg = seg_heads / 32;
     for (int h0 = warp * span; h0 < p.heads; h0 += kWarpsAll * span) {
-      Counts mine = {};
+      int mine = 0;
       for (int i = h0; i < h0 + span; i += 512) {
         int len[16];  // sixteen loads at once
 #pragma unroll
@@ -867,22 +876,30 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         }
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          if (len[j] >= 0) mine.add(Counts::of<S>(len[j]));
+          if (len[j] >= 0) mine += see(len[j]).boxes;
           const int h = i + 32 * j;
           if (((h / 32 + 1) & (per_seg - 1)) == 0) {
-            const Counts sum = mine.over_warp();
-            if (lane == 0 && h - (seg_heads - 32) < p.heads) sh.segs[h / seg_heads] = sum;
-            mine = Counts{};
+            const int sum = __reduce_add_sync(0xffffffffu, mine);
+            if (lane == 0 && h - (seg_heads - 32) < p.heads) sh.segs[h / seg_heads] = Counts{sum, 0, 0};
+            mine = 0;
           }
         }
       }
     }
   }
+  most = __reduce_max_sync(0xffffffffu, most);
+  empty = __reduce_add_sync(0xffffffffu, empty);
+  if (lane == 0) sh.seen[warp] = make_int2(most, empty);
   __syncthreads();
   Counts all = {};
   for (int seg = lane; seg * seg_heads < p.heads; seg += 32) all.add(sh.segs[seg]);
   all = all.over_warp();
-  if (all.empty)  // zeros for heads without rows
+#pragma unroll
+  for (int w = 0; w < kWarpsAll; ++w) {
+    most = max(most, sh.seen[w].x);
+    empty |= sh.seen[w].y;
+  }
+  if (empty)  // zeros for heads without rows
     for (int h = blockIdx.x + tid * gridDim.x; h < p.heads; h += kThreads * gridDim.x) {
       if (head_len(p, h) > 0) continue;
       const size_t row = first_query(c, h);
@@ -890,7 +907,7 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
       if (p.lse)
         for (int e = 0; e < c.group; ++e) p.lse[row + e] = -INFINITY;
     }
-  const Plan plan = plan_of<S>(p, all);
+  const Plan plan = plan_of<S>(p, all, most);
   if ((int)blockIdx.x >= plan.parts) return;
 
   if (plan.by_warp) {
@@ -916,25 +933,22 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   }
   Part part;
   {
+    // the piece, or the box, that this CTA's part begins with
     const int unit = plan.piece ? (int)blockIdx.x : part_begin(plan.total, plan.parts, blockIdx.x);
-    const auto counted = [&](const Counts& x) {
-      return (plan.piece == S::kSmall ? x.small : plan.piece ? x.large : x.tiles) * p.subs;
-    };
-    const int2 f = find_unit<S>(p, sh.segs, seg_heads, unit, counted);
-    const Counts its = Counts::of<S>(head_len(p, f.x));
-    const int tiles = its.tiles, n = plan.piece == S::kSmall ? its.small : plan.piece ? its.large : tiles;
+    const int2 f = find_unit<S>(p, sh.segs, seg_heads, unit, [&](const Counts& x) {
+      return (plan.piece == S::kSmall ? x.small : plan.piece ? x.large : x.boxes) * p.subs;
+    });
+    const int len = head_len(p, f.x), tiles = tiles_of<S>(len);
+    const Counts its = Counts::of<S>(len);
+    const int n = plan.piece == S::kSmall ? its.small : plan.piece ? its.large : its.boxes;
     const int sub = p.subs == 1 ? 0 : (unit - f.y) / n, i = unit - f.y - sub * n;
-    part.head = f.x;
-    part.sub = sub;
     if (plan.piece) {
-      part.tile = n == 1 ? 0 : part_begin(tiles, n, i);
-      part.tiles = n == 1 ? tiles : part_begin(tiles, n, i + 1) - part.tile;
-      part.first = unit - i;
-      part.pieces = n;
+      // (a line of its own, which ends with the piece)
+      const int t0 = n == 1 ? 0 : part_begin(tiles, n, i), t1 = n == 1 ? tiles : part_begin(tiles, n, i + 1);
+      part = {f.x, sub, t0, 0, min(its.boxes, t1 * kBoxesOf<S>), unit - i, n};
     } else {
-      part.tile = i;
-      part.tiles = part_begin(plan.total, plan.parts, blockIdx.x + 1) - unit;
-      part.first = part.pieces = 0;
+      // the first tile that begins there or behind it: it may be the next portion's
+      part = {f.x, sub, (i + kBoxesOf<S> - 1) / kBoxesOf<S>, f.y + sub * n, part_begin(plan.total, plan.parts, blockIdx.x + 1), 0, 0};
     }
   }
   const auto wait = [&](uint64_t* bar, int parity) {  // the same in all lanes
@@ -947,17 +961,20 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
       parity ^= 1;
     }
   };
-  int h = part.head, sub = part.sub, t0 = part.tile, done = 0;  // t0: of the portion in hand; done: tiles of the part
+  // the portion in hand: its head, where it begins on the line, its first tile that is this CTA's
+  int h = part.head, sub = part.sub, at0 = part.at, t0 = part.tile;
 
   if (warp == kConsumers) {
     // ---- producer ----------------------------------------------------------------------------------
-    constexpr int kBoxes = S::kTile / kBoxRows, kAhead = 32 / kBoxes;
+    constexpr int kBoxes = kBoxesOf<S>, kAhead = 32 / kBoxes;
+    int done = 0;  // tiles
     bool alive = true;
-    for (; done < part.tiles && alive && h < p.heads; ++h, sub = 0) {
-      const int len = head_len(p, h), n = tiles_of<S>(len);
+    for (; at0 < part.end && alive && h < p.heads; ++h, sub = 0) {
+      const int len = head_len(p, h), n = tiles_of<S>(len), boxes_of = (len + kBoxRows - 1) / kBoxRows;
       if (n == 0) continue;
-      for (; sub < p.subs && done < part.tiles && alive; ++sub, t0 = 0) {
-        const int tiles = min(n - t0, part.tiles - done);
+      for (; sub < p.subs && at0 < part.end && alive; ++sub, t0 = 0, at0 += boxes_of) {
+        const int tiles = min(n, (part.end - at0 + kBoxes - 1) / kBoxes) - t0;
+        if (tiles <= 0) continue;
         int places = 0;
         for (int t = 0; t < tiles; ++t) {
           if (t % kAhead == 0) {  // the places of the next 32 boxes, a lane each
@@ -991,11 +1008,13 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     float* const probs = sh.probs[BF16 ? 0 : warp];
     int fetched = -1;  // the head whose queries are on their way
     bool alive = true, begun = false, ended = false;  // others have tiles of the portion that the part begins, ends in
-    for (; done < part.tiles && alive && h < p.heads; ++h, sub = 0) {
-      const int len = head_len(p, h), n = tiles_of<S>(len);
+    for (; at0 < part.end && alive && h < p.heads; ++h, sub = 0) {
+      const int len = head_len(p, h), n = tiles_of<S>(len), boxes_of = (len + kBoxRows - 1) / kBoxRows;
       if (n == 0) continue;
-      for (; sub < p.subs && done < part.tiles; ++sub, t0 = 0) {
-        const int tiles = min(n - t0, part.tiles - done), queries = min(p.per_sub, c.group - sub * p.per_sub);
+      for (; sub < p.subs && at0 < part.end; ++sub, t0 = 0, at0 += boxes_of) {
+        const int tiles = min(n, (part.end - at0 + kBoxesOf<S> - 1) / kBoxesOf<S>) - t0;
+        if (tiles <= 0) continue;
+        const int queries = min(p.per_sub, c.group - sub * p.per_sub);
         if (fetched != h) w.fetch(p, first_query(c, h) + sub * p.per_sub, queries);
         w.begin(q_mem);
         if (p.subs == 1) {  // the next head's, in case it follows
@@ -1050,9 +1069,8 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
           if (tid == 0) {  // the CTAs that have tiles of the portion
             Pending x = {part.first, part.pieces, queries, q_row};
             if (!plan.piece) {
-              const int at = part_begin(plan.total, plan.parts, blockIdx.x) + done - t0;  // the portion's first tile
-              x.w0 = part_of(plan.total, plan.parts, at);
-              x.n = part_of(plan.total, plan.parts, at + n - 1) + 1 - x.w0;
+              x.w0 = part_of(plan.total, plan.parts, at0);
+              x.n = part_of(plan.total, plan.parts, at0 + (n - 1) * kBoxesOf<S>) + 1 - x.w0;
             }
             sh.pending[t0 == 0] = x;
           }
@@ -1061,7 +1079,6 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         meet();
         if (lane == 0) mbar_arrive(smem_u32(&sh.empty[stage]));
         next_stage();
-        done += tiles;
       }
     }
     // Portions that other CTAs have tiles of, when the part is through: who comes last joins them.

@@ -157,6 +157,17 @@ def test_long_heads_and_large_groups(rows, group, dtype):
     _check(rows, group=group, d=64, dtype=dtype)
 
 
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.float32, 128), (torch.bfloat16, 64)])
+@pytest.mark.parametrize("n_heads", [1, 3, 40, 1024, 1030, 2100])
+def test_heads_of_odd_numbers_of_boxes(dtype, d, n_heads):
+    """Heads whose last tile is not full, one after the other on the line: every cut falls elsewhere in a tile."""
+    g = np.random.default_rng(n_heads)
+    rows = g.choice([1, 17, 33, 49, 65, 79, 161, 300], (n_heads, 1, 1))
+    if n_heads > 1000:
+        rows[n_heads // 3] = 9001                                    # too long for whole heads per warp
+    _check(rows.tolist(), group=2, d=d, dtype=dtype, page_rows=16)
+
+
 def test_first_rows_at_minus_infinity_over_many_tiles():
     """-inf logits fill whole tiles, pieces and parts before the first finite one."""
     c = Case([[[3000, 40]]], group=2, dtype=torch.float32, d=64)
