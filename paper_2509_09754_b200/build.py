@@ -1,4 +1,5 @@
-"""Builds liblava.so (sm_100a) in-tree with nvcc.  `python -m paper_2509_09754_b200.build`."""
+"""Builds liblava.so (sm_100a) with nvcc and the paged cache's calls from Python with g++, both in-tree.
+`python -m paper_2509_09754_b200.build`."""
 from __future__ import annotations
 
 import os
@@ -10,6 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB_DIR = os.path.join(PKG, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "liblava.so")
+CALLS_PATH = os.path.join(LIB_DIR, "_paged_calls.so")
 
 SOURCES = ["lava_api.cu", "score_generic.cu", "budgets.cu", "select.cu", "compact.cu",
            "host_path.cu", "score_sm100.cu", "score_tmem.cu", "score_variants.cu", "cascade.cu", "loss_eval.cu", "decode.cu", "select_shard.cu", "score_static.cu",
@@ -56,7 +58,31 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         cmd = [_nvcc(), "-shared", "-o", LIB_PATH] + objs + ["-gencode",
                "arch=compute_100a,code=sm_100a", "-cudart", "static"]
         subprocess.run(cmd, check=True)
+    build_calls(force, verbose)
     return LIB_PATH
+
+
+def build_calls(force: bool = False, verbose: bool = False) -> str:
+    """Compile csrc/paged_calls.cpp into the module that paged.py loads; returns its path."""
+    import sysconfig
+    import torch
+    src, header = os.path.join(CSRC, "paged_calls.cpp"), os.path.join(ROOT, "include", "lava.h")
+    home = os.path.dirname(torch.__file__)
+    if force or _stale(CALLS_PATH, [src, header, os.path.join(home, "version.py")]):
+        cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
+        cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
+               "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+        for inc in (os.path.join(ROOT, "include"), os.path.join(home, "include"),
+                    os.path.join(home, "include", "torch", "csrc", "api", "include"),
+                    sysconfig.get_paths()["include"], os.path.join(cuda, "include")):
+            cmd += ["-I", inc]
+        # torch's libraries are in the process already when the module is loaded
+        cmd += [src, "-o", CALLS_PATH, "-L", LIB_DIR, "-llava", "-Wl,-rpath,$ORIGIN", "-L", os.path.join(home, "lib"),
+                "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+        if verbose:
+            print(" ".join(cmd))
+        subprocess.run(cmd, check=True)
+    return CALLS_PATH
 
 
 if __name__ == "__main__":

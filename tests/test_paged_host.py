@@ -11,6 +11,7 @@ import torch
 import paper_2509_09754_b200 as lava
 from oracle import paged_oracle as PO
 from paper_2509_09754_b200 import binding
+from paper_2509_09754_b200 import paged as P
 
 GOOD = dict(n_layers=2, batch=3, n_q_heads=8, n_kv_heads=2, head_dim=64, max_pages=4, n_pages=64, page_rows=16)
 
@@ -256,6 +257,46 @@ def test_tensors_that_do_not_fit_are_refused_before_the_library_sees_them():
     refused(lava.lava_rotary, rot, f, pos, x, None, x.transpose(1, 2), None)
     refused(lava.lava_rotary, rot, f.float(), pos, x, None, x, None)
     refused(lava.lava_rotary_append, rot, f, c, 2, pos, x, x[:, :2], x[:, :2], x.clone(), slots, pool, pool)
+
+
+def test_arguments_of_another_kind_are_refused():
+    """What is no tensor, no number in range or no stream is an exception, whatever comes after it."""
+    c = _cache()
+    rot = lava.RotaryDesc(head_dim=64, rotary_dim=64)
+    L, B, H = 2, 3, 2
+    table = torch.zeros((L, B, H, 4), dtype=torch.int32)
+    rows = torch.zeros((L, B, H), dtype=torch.int32)
+    pool = torch.zeros((64, 16, 64), dtype=torch.bfloat16)
+    q = torch.zeros((1, B, 8, 64), dtype=torch.bfloat16)
+    ws = torch.zeros(lava.lava_cache_workspace_bytes(c), dtype=torch.uint8)
+    for x in (None, 7, "q", [1.0], object()):
+        with pytest.raises(lava.LavaError) as e:
+            lava.lava_decode_attention_pages(c, 0, x, pool, pool, table, rows, q, None, ws)
+        assert e.value.status == 1 and "q must be a tensor" in str(e.value)
+        with pytest.raises(lava.LavaError):
+            lava.lava_rotary(rot, x, None, None, None, None, None)
+        with pytest.raises(lava.LavaError):
+            lava.lava_page_extend(c, x, rows, table, x, x, x)
+    for n in (1 << 31, -(1 << 31) - 1, 1 << 63, -(1 << 70)):
+        with pytest.raises(lava.LavaError) as e:
+            lava.lava_decode_attention_pages(c, n, q, pool, pool, table, rows, q, None, ws)
+        assert "first_layer is out of range" in str(e.value)
+    with pytest.raises(TypeError):
+        lava.lava_decode_attention_pages(c, 0.5, q, pool, pool, table, rows, q, None, ws)
+    with pytest.raises(TypeError):
+        P.load_paged_calls().rotary(1, 2, 3)
+    with pytest.raises(lava.LavaError):
+        P.load_paged_calls().rotary(*[0] * 8)          # a descriptor that is NULL
+    with pytest.raises(lava.LavaError):                # a tensor without memory
+        lava.lava_decode_attention_pages(c, 0, q.to("meta"), pool, pool, table, rows, q, None, ws)
+
+
+def test_a_missing_module_of_calls_is_an_error(monkeypatch, tmp_path):
+    lib = tmp_path / "liblava.so"
+    monkeypatch.setattr(P, "library_path", lambda: str(lib))
+    monkeypatch.setattr(P, "_CALLS", None)
+    with pytest.raises(RuntimeError, match="_paged_calls.so is missing"):
+        P.load_paged_calls()
 
 
 def test_oracle_tables():
