@@ -412,7 +412,8 @@ LAVA_API size_t lava_cache_workspace_bytes(const lava_cache_desc* cache);
  * suffice or a count does not fit.
  *   lava_page_admit   the selection of new prompts: sequences first_seq ... first_seq + n_seqs - 1
  *       of the cache get head_offsets[l][s][g+1] - head_offsets[l][s][g] more rows (head_offsets
- *       [n_layers, n_seqs, H_kv+1] as written by lava_select_topk_layers).
+ *       [n_layers, n_seqs, H_kv+1] as written by lava_select_topk_layers.  That leaves them as they were
+ *       where a sequence is shorter than the window: zeros there before it admit nothing then).
  *       first_row   out int32 [n_layers, n_seqs, H_kv]: where a head's new rows start
  *   lava_page_extend  a decode step: every head of sequence b gets add[b] more rows (device int32
  *       [batch], 0 ... max_add), or, where add[b] < 0, gives all its pages back and holds no rows.
@@ -479,7 +480,8 @@ LAVA_API lava_status lava_rotary_freqs(int32_t kind, int32_t rotary_dim, double 
 /* Queries and keys of n_tokens tokens, each [tokens][heads][head_dim] by its own strides in elements
  * (out strides may differ from in strides: the output can be laid out as lava_score_layer reads it).
  * positions: device int32 [n_tokens]; freqs: DEVICE double [rotary_dim/2].  q and q_out, or k and k_out,
- * may both be NULL.  An output may be its own input (same pointer and strides), else it overlaps no input. */
+ * may both be NULL.  An output may be its own input (same pointer and strides), else it overlaps no input;
+ * the outputs do not overlap each other. */
 LAVA_API lava_status lava_rotary(const lava_rotary_desc* rotary, const double* freqs, int64_t n_tokens,
                                  const int32_t* positions,
                                  const void* q, int32_t n_q_heads, int64_t q_stride_tok, int64_t q_stride_head,
@@ -506,7 +508,7 @@ LAVA_API lava_status lava_rotary_append(const lava_rotary_desc* rotary, const do
  *     x_i = sm_scale * q[h] . K_g[i]   (capped where softcap > 0),   i < head_rows
  *     out[h] = softmax_i(x_i) V_g,     lse[h] = ln sum_i exp(x_i)
  * for layers first_layer ... first_layer + n_layers - 1 in one call.
- *   q, out      [n_layers, batch, H_q, d], dtype cache->dtype
+ *   q, out      [n_layers, batch, H_q, d], dtype cache->dtype; they must not overlap
  *   lse         float [n_layers, batch, H_q], may be NULL
  *   page_table, head_rows   of the whole cache
  *   workspace   lava_cache_workspace_bytes(cache) bytes, zeroed once

@@ -1182,6 +1182,10 @@ lava_status lava_decode_attention_pages(const lava_cache_desc* cache, int32_t fi
   const Portions portions = portions_of(c);
   if ((long long)n_layers * c.batch * c.n_kv_heads * portions.subs >= (1ll << 35) / ((long long)c.max_pages << c.page_shift))
     return fail(LAVA_ERR_UNSUPPORTED, "too many rows in one call: heads * max_pages * page_rows must stay below 2^35");
+  // blocks read queries while others write outputs
+  const size_t io_bytes = (size_t)n_layers * c.batch * c.n_q_heads * c.head_dim * (c.dtype == LAVA_BF16 ? 2 : 4);
+  if ((const char*)q < (const char*)out + io_bytes && (const char*)out < (const char*)q + io_bytes)
+    return fail(LAVA_ERR_INVALID_ARG, "out overlaps q");
   CUtensorMap map_k, map_v;
   rc = encode_pages_map(c, k_pages, &map_k);
   if (rc == LAVA_OK) rc = encode_pages_map(c, v_pages, &map_v);

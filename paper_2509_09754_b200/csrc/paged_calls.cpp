@@ -233,17 +233,20 @@ PyObject* compact_kv_pages(PyObject* const* args, Py_ssize_t n) {
   const int64_t L = d->n_layers, H = d->n_kv_heads, D = d->head_dim, T = layer->total_tokens, S = layer->batch;
   const at::ScalarType type = type_of(d->dtype);
   const char* names[2] = {"k", "v"};
-  const void* kv[2] = {};
+  const int64_t by_head[2] = {layer->k_stride_head, layer->v_stride_head}, by_tok[2] = {layer->k_stride_tok, layer->v_stride_tok};
+  const at::Tensor* kv[2] = {};
   for (int i = 0; i < 2; ++i) {
-    const at::Tensor* t = c.tensor(names[i]);
+    const at::Tensor* t = kv[i] = c.tensor(names[i]);
     if (!t) return nullptr;
     if (t->scalar_type() != type || t->sizes() != at::IntArrayRef({L, H, T, D}) || t->stride(3) != 1 || !c.here(*t))
       c.refuse(std::string(names[i]) + " must be a " + c10::toString(type) + " tensor of shape " + shape_text({L, H, T, D}) +
                " with contiguous rows, on the current device");
-    else
-      kv[i] = t->data_ptr();
+    else if ((H > 1 && t->stride(1) != by_head[i]) || (T > 1 && t->stride(2) != by_tok[i]))
+      c.refuse(std::string(names[i]) + " does not have the strides that desc names");
   }
   const long long k_ls = c.integer("k_layer_stride", INT64_MAX), v_ls = c.integer("v_layer_stride", INT64_MAX);
+  if (!c.ok()) return nullptr;
+  if (L > 1 && (kv[0]->stride(0) != k_ls || kv[1]->stride(0) != v_ls)) c.refuse("the layer strides are not those of k and v");
   const auto* keep = (const int32_t*)c.buffer("keep_idx", at::kInt, {L, layer->n_kv_heads * (T - S * layer->window)});
   const auto* hoff = (const int32_t*)c.buffer("head_offsets", at::kInt, {L, S, H + 1});
   const auto* first_row = (const int32_t*)c.buffer("first_row", at::kInt, {L, S, H});
@@ -252,8 +255,9 @@ PyObject* compact_kv_pages(PyObject* const* args, Py_ssize_t n) {
   void* v_pages = c.buffer("v_pages", type, {d->n_pages, d->page_rows, D});
   void* stream = c.stream();
   if (!c.ok()) return nullptr;
+  const void *k = kv[0]->data_ptr(), *v = kv[1]->data_ptr();
   return finish([&] {
-    return lava_compact_kv_pages(layer, d, first_seq, kv[0], kv[1], k_ls, v_ls, keep, hoff, first_row, table, k_pages,
+    return lava_compact_kv_pages(layer, d, first_seq, k, v, k_ls, v_ls, keep, hoff, first_row, table, k_pages,
                                  v_pages, stream);
   });
 }

@@ -315,6 +315,8 @@ page_table_kernel(const __grid_constant__ TableParams p) {
 }
 
 lava_status launch_tables(const TableParams& p, cudaStream_t stream) {
+  if (reinterpret_cast<uintptr_t>(p.status) % 4 != 0)  // (it may be a word in a buffer of bytes)
+    return fail(LAVA_ERR_INVALID_ARG, "status_word must be 4-byte aligned");
   // a CTA for every 128 heads and a thread per head, then more threads, then more heads per thread
   int ctas = 1;
   while (ctas < kMostCtas && ctas * 128 < p.c.heads) ctas *= 2;

@@ -44,6 +44,14 @@ def _handle(stream):
     return None if stream is None else stream.cuda_stream
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory for work on this stream: torch hands it out, and takes it back, in the order of the stream's work."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 @dataclass(frozen=True)
 class CacheDesc:
     """Geometry of a paged cache (lava_cache_desc of the C ABI)."""
@@ -199,24 +207,27 @@ class PagedCache:
         """The selection of a plan (its keep_idx and head_offsets) as sequences first_seq ... of the cache: pages, and
         the kept rows of k and v [n_layers, H_kv, total_tokens, d] in them, behind what the sequences hold."""
         d = self.desc
-        first_row = torch.empty((d.n_layers, plan.desc.batch, d.n_kv_heads), dtype=torch.int32,
-                                device=self.head_rows.device)
+        first_row = _empty((d.n_layers, plan.desc.batch, d.n_kv_heads), torch.int32, self.head_rows.device, stream)
         lava_page_admit(d, first_seq, plan.head_offsets, self.head_rows, self.page_table, self.free_pages,
                         self.counters, first_row, self.workspace, stream=stream)
         lava_compact_kv_pages(plan.desc, d, first_seq, k, v, k.stride(0), v.stride(0), plan.keep_idx,
                               plan.head_offsets, first_row, self.page_table, self.k_pages, self.v_pages, stream)
 
     def evict(self, plan: EvictionPlan, q_win, k, v, first_seq: int = 0, mode: int = 0, stream=None) -> None:
-        """evict_model with the kept rows in the pages of this cache instead of the plan's packed cache."""
+        """evict_model with the kept rows in the pages of this cache instead of the plan's packed cache.  A batch with a
+        sequence shorter than the window is left alone as there (the plan's status word says so): nothing enters."""
+        with torch.cuda.stream(stream):
+            plan.head_offsets.zero_()  # (the selection of such a batch writes none)
         evict_scores(plan, q_win, k, v, mode, stream)
         self.admit(plan, k, v, first_seq, stream)
 
     def extend(self, add, max_add: int = 1, stream=None) -> torch.Tensor:
-        """Room for add[b] new rows in every head of sequence b, -1 releases it; the rows' places."""
+        """Room for add[b] new rows in every head of sequence b, -1 releases it; the rows' places (in memory of the
+        cache's own, which `append` reads and the next call writes)."""
         d = self.desc
         shape = (d.n_layers, d.batch, max_add, d.n_kv_heads)
         if self.slots is None or self.slots.shape != shape:
-            self.slots = torch.empty(shape, dtype=torch.int32, device=self.head_rows.device)
+            self.slots = _empty(shape, torch.int32, self.head_rows.device, stream)
         lava_page_extend(d, add, self.head_rows, self.page_table, self.free_pages, self.counters, self.slots,
                          self.workspace, stream=stream)
         return self.slots
@@ -226,7 +237,7 @@ class PagedCache:
         if self.slots is None:
             raise LavaError(1, "append without extend")
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = _empty(q.shape, q.dtype, q.device, stream)
         lava_rotary_append(rotary, freqs, self.desc, layer, positions, q, k, v, q_out, self.slots, self.k_pages,
                            self.v_pages, stream)
         return q_out
@@ -235,8 +246,8 @@ class PagedCache:
         """(out, lse) of q [batch, H_q, d] or [n_layers, batch, H_q, d] over the rows that the heads hold."""
         one = q.dim() == 3
         q = q.unsqueeze(0) if one else q
-        out = torch.empty_like(q) if out is None else out.view(q.shape)
-        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if lse is None else lse.view(q.shape[:3])
+        out = _empty(q.shape, q.dtype, q.device, stream) if out is None else out.view(q.shape)
+        lse = _empty(q.shape[:3], torch.float32, q.device, stream) if lse is None else lse.view(q.shape[:3])
         lava_decode_attention_pages(self.desc, first_layer, q, self.k_pages, self.v_pages, self.page_table,
                                     self.head_rows, out, lse, self.workspace, stream)
         return (out[0], lse[0]) if one else (out, lse)

@@ -164,3 +164,80 @@ def test_a_prompt_that_finds_no_pages_leaves_the_cache_as_it_was():
     cache.extend(torch.tensor([-1, 0], dtype=torch.int32, device="cuda"))
     cache.evict(plan, q, k, v, first_seq=1)
     assert cache.poll_status() == 0 and int(cache.head_rows[0, 1].sum()) == 128
+
+
+def _cache_of(cfg, batch, dt, **kw):
+    return lava.PagedCache(lava.CacheDesc(n_layers=cfg.n_layers, batch=batch, n_q_heads=cfg.n_q_heads,
+                                          n_kv_heads=cfg.n_kv_heads, head_dim=cfg.head_dim,
+                                          dtype=lava.LAVA_BF16 if dt == torch.bfloat16 else lava.LAVA_F32,
+                                          **dict(dict(page_rows=32, max_pages=40, n_pages=4000), **kw)))
+
+
+@pytest.mark.parametrize("name", ["mistral7b_ragged", "tiny"])
+def test_a_batch_with_a_prompt_shorter_than_the_window_does_not_enter(name):
+    """Nothing of such a batch is scored or selected, and the plan still has the offsets of the batch before."""
+    cfg = get_config(name).scaled(seq_lens=(300, 333), n_layers=2, budget_per_head=40)
+    q, k, v, cu = upload_model(cfg)
+    plan = make_plan(cfg, q, k, v, cu)
+    cache = _cache_of(cfg, 4, k.dtype)
+    cache.evict(plan, q, k, v)
+    # (40 entries per head are less than the one window: LAVA_DEV_BUDGET_INFEASIBLE says that they were clamped)
+    assert lava.lava_poll_status(plan.workspace) & ~2 == 0 and int(cache.head_rows[:, :2].min()) > 0
+    rows, free, table = cache.head_rows.clone(), cache.free_page_count(), cache.page_table.clone()
+    pages = cache.k_pages.clone()
+    short = cfg.window // 2
+    cu.copy_(torch.tensor([0, short, 333], dtype=torch.int32))
+    cache.evict(plan, q, k, v, first_seq=2)
+    assert lava.lava_poll_status(plan.workspace) & 1    # LAVA_DEV_SHORT_SEQUENCE
+    assert torch.equal(cache.head_rows, rows) and cache.free_page_count() == free
+    assert torch.equal(cache.page_table, table)
+    # (untouched memory may hold NaN: compared as bits)
+    assert torch.equal(cache.k_pages.view(torch.uint8), pages.view(torch.uint8))
+
+
+def test_a_stream_of_its_own():
+    """All of a cache's work on a stream that is not the current one, which allocates and writes meanwhile: what the
+    calls allocate belongs to their stream."""
+    cfg = get_config("mistral7b_ragged").scaled(seq_lens=(640, 901), n_layers=2, budget_per_head=96)
+    q, k, v, cu = upload_model(cfg)
+    freqs = lava.lava_rotary_freqs(cfg.head_dim, 10000.0)[0].cuda()
+    rotary = lava.RotaryDesc(head_dim=cfg.head_dim, rotary_dim=cfg.head_dim)
+    gen = torch.Generator().manual_seed(5)
+    new = {n: torch.randn((2, h, cfg.head_dim), generator=gen).bfloat16().cuda()
+           for n, h in (("q", cfg.n_q_heads), ("k", cfg.n_kv_heads), ("v", cfg.n_kv_heads))}
+    at, add = torch.tensor([640, 901], dtype=torch.int32).cuda(), torch.ones(2, dtype=torch.int32).cuda()
+    got = []
+    for own in (False, True):
+        plan = make_plan(cfg, q, k, v, cu)
+        cache = _cache_of(cfg, 2, k.dtype)
+        cache.k_pages.zero_()
+        stream = torch.cuda.Stream() if own else None
+        torch.cuda.synchronize()
+        cache.evict(plan, q, k, v, stream=stream)
+        junk = [torch.full((2, 2, cfg.n_kv_heads), 1 << 30, dtype=torch.int32, device="cuda") for _ in range(8)]
+        cache.extend(add, stream=stream)
+        outs = []
+        for l in range(2):
+            turned = cache.append(rotary, freqs, l, at, new["q"], new["k"], new["v"], stream=stream)
+            outs.append((turned, *cache.attend(l, turned, stream=stream)))
+            junk.append(torch.full_like(new["q"], 7.0))
+        torch.cuda.synchronize()
+        assert cache.poll_status() == 0 and len(junk) == 10
+        got.append([x.clone() for o in outs for x in o] + [cache.head_rows, cache.page_table, cache.k_pages])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_strides_that_desc_does_not_name_are_refused():
+    cfg = get_config("tiny").scaled(seq_lens=(300,), n_layers=2, budget_per_head=40)
+    q, k, v, cu = upload_model(cfg)
+    plan = make_plan(cfg, q, k, v, cu)
+    cache = _cache_of(cfg, 1, k.dtype)
+    cache.evict(plan, q, k, v)
+    first_row = torch.zeros((2, 1, cfg.n_kv_heads), dtype=torch.int32, device="cuda")
+    wide = torch.zeros((*k.shape[:3], 2 * k.shape[3]), dtype=k.dtype, device="cuda")[..., : k.shape[3]]
+    for kk, vv in ((wide, v), (k, wide), (k[:, :, :1].expand(k.shape), v), (k[:1].expand(k.shape), v),
+                   (k, v[:, :1].expand(v.shape))):
+        with pytest.raises(lava.LavaError) as e:
+            lava.lava_compact_kv_pages(plan.desc, cache.desc, 0, kk, vv, k.stride(0), v.stride(0), plan.keep_idx,
+                                       plan.head_offsets, first_row, cache.page_table, cache.k_pages, cache.v_pages)
+        assert e.value.status == 1 and "strides" in str(e.value)

@@ -57,6 +57,25 @@ def test_bad_arguments_of_page_tables_are_refused():
         assert lib.lava_page_admit(c._ref, 0, 1, *ptrs, None, None) == 1
 
 
+def test_a_status_word_that_is_not_aligned_is_refused():
+    """(It may be a view of a buffer of bytes.)"""
+    lib = lava.load_library()
+    c, p = _cache(), 256
+    for off in (1, 2, 3):
+        assert lib.lava_page_extend(c._ref, p, 1, p, p, p, p, p, p, p, p + off, None) == 1
+        assert lib.lava_page_admit(c._ref, 0, 1, p, p, p, p, p, p, p, p, p + off, None) == 1
+        assert "aligned" in lava.lava_last_error()
+
+
+def test_outputs_of_the_attention_that_overlap_its_queries_are_refused():
+    lib = lava.load_library()
+    c, p, q = _cache(), 256, 1 << 20
+    need, size = lava.lava_cache_workspace_bytes(c), 2 * 3 * 8 * 64 * 2  # of 2 layers, 3 sequences, 8 heads
+    for out in (q, q + 16, q - 16, q + size - 16, q - size + 16):
+        assert lib.lava_decode_attention_pages(c._ref, 0, 2, q, p, p, p, p, out, None, p, need, None) == 1
+        assert "overlaps" in lava.lava_last_error()
+
+
 def _layer_desc(**kw):
     base = dict(n_q_heads=8, n_kv_heads=2, head_dim=64, window=16, total_tokens=512, k_stride_head=512 * 64,
                 k_stride_tok=64, v_stride_head=512 * 64, v_stride_tok=64)
