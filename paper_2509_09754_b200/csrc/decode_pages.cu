@@ -337,8 +337,16 @@ struct PlainWarp {
   static constexpr int kQueryBytes = Q * D * 4;
   static constexpr int kNext = Q * D / 4 / (kOwnQueries ? 32 : 32 * kConsumers);
   static_assert(kNext >= 1, "a lane has a piece of the queries");
+  // The lanes that share a row split the queries when its logits are summed: each has kOwn of them, from own0() on.
+  static constexpr int kOwn = Q / kSplit;
+  static_assert(kOwn >= 1 && kOwn * kSplit == Q, "queries of a lane");
   uint4 next[kNext];      // of the queries of the next head
-  float m[Q], l[Q], o[Q][kCols];
+  float m[kOwn], l[kOwn], o[Q][kCols];
+  static __device__ __forceinline__ int own0() { return (threadIdx.x & 31) / kRows * kOwn; }
+  // query q's value among those that the lanes have of their own (the same for all rows)
+  static __device__ __forceinline__ float of_query(const float (&x)[kOwn], int q) {
+    return __shfl_sync(0xffffffffu, x[q % kOwn], q / kOwn * kRows);
+  }
 
   __device__ __forceinline__ void fetch(const PageParams& p, size_t q_row, int queries) {
     const int first = kOwnQueries ? threadIdx.x & 31 : threadIdx.x;
@@ -358,12 +366,14 @@ struct PlainWarp {
     if (kOwnQueries) __syncwarp();
     else meet();
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      m[q] = -INFINITY;
-      l[q] = 0.f;
+    for (int i = 0; i < kOwn; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
       for (int c = 0; c < kCols; ++c) o[q][c] = 0.f;
-    }
   }
 
   __device__ __forceinline__ void tile(uint32_t k_tile, uint32_t v_tile, int r0, int valid, const Logit& logit,
@@ -383,28 +393,47 @@ struct PlainWarp {
         z[q] = fmaf(a.x, k.x, fmaf(a.y, k.y, fmaf(a.z, k.z, fmaf(a.w, k.w, z[q]))));
       }
     }
-    float corr[Q];
+    // sums over the lanes of a row, which halve their queries at every step
+    int left = Q;
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
+    for (int w = 16; w >= kRows; w /= 2) {
+      left /= 2;
+      const bool upper = lane & w;
 #pragma unroll
-      for (int w = kRows; w < 32; w *= 2) z[q] += __shfl_xor_sync(0xffffffffu, z[q], w);
-      z[q] = row < valid ? logit.of(z[q]) : -INFINITY;
-      float best = z[q];
+      for (int i = 0; i < Q / 2; ++i)
+        if (i < left) {
+          const float away = upper ? z[i] : z[left + i], mine = upper ? z[left + i] : z[i];
+          z[i] = mine + __shfl_xor_sync(0xffffffffu, away, w);
+        }
+    }
+    float corr[kOwn];
+    bool moved = false;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      z[i] = row < valid ? logit.of(z[i]) : -INFINITY;
+      float best = z[i];
 #pragma unroll
       for (int w = 1; w < kRows; w *= 2) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, w));
-      const float m_new = fmaxf(m[q], best), ref = finite_ref(m_new);
-      corr[q] = fast_exp2(m[q] - ref);
-      m[q] = m_new;
-      z[q] = fast_exp2(z[q] - ref);
-      l[q] = l[q] * corr[q] + (share == 0 ? z[q] : 0.f);  // a lane's own rows
+      const float m_new = fmaxf(m[i], best), ref = finite_ref(m_new);
+      corr[i] = fast_exp2(m[i] - ref);
+      moved |= m_new != m[i];
+      m[i] = m_new;
+      z[i] = fast_exp2(z[i] - ref);
+      l[i] = l[i] * corr[i] + z[i];  // a lane's own rows
+    }
+    if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-      for (int c = 0; c < kCols; ++c) o[q][c] *= corr[q];
+      for (int q = 0; q < Q; ++q) {
+        const float x = of_query(corr, q);
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) o[q][c] *= x;
+      }
     }
     __syncwarp();  // (the probabilities of the tile before have been read)
-    if (share == 0)
-#pragma unroll
-      for (int q = 0; q < Q; q += 4)
-        *reinterpret_cast<float4*>(probs + row * Q + q) = make_float4(z[q], z[q + 1], z[q + 2], z[q + 3]);
+    float* const to = probs + row * Q + own0();
+    if constexpr (kOwn == 4) *reinterpret_cast<float4*>(to) = make_float4(z[0], z[1], z[2], z[3]);
+    else if constexpr (kOwn == 2) *reinterpret_cast<float2*>(to) = make_float2(z[0], z[1]);
+    else to[0] = z[0];
     __syncwarp();
 #pragma unroll 4
     for (int r = 0; r < kRows; ++r) {
@@ -430,13 +459,18 @@ struct PlainWarp {
     }
   }
 
+  // sums of the lanes' rows
+  __device__ __forceinline__ void sum_rows() {
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+#pragma unroll
+      for (int w = 1; w < kRows; w *= 2) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
+  }
   __device__ __forceinline__ void leave_stats(float2* ml) {
+    sum_rows();
+    if ((threadIdx.x & 31) % kRows == 0)
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-#pragma unroll
-      for (int w = 16; w > 0; w >>= 1) l[q] += __shfl_xor_sync(0xffffffffu, l[q], w);
-      if ((threadIdx.x & 31) == 0) ml[q] = make_float2(m[q], l[q]);
-    }
+      for (int i = 0; i < kOwn; ++i) ml[own0() + i] = make_float2(m[i], l[i]);
   }
   // where in a stage warp i leaves four columns from `col` on of query q: in its own box of K; or, where a box is two
   // warps', in the q-th of its own rows
@@ -455,15 +489,15 @@ struct PlainWarp {
   }
   __device__ __forceinline__ void finish(const PageParams& p, size_t q_row, int queries) {
     const int lane = threadIdx.x & 31;
+    sum_rows();
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-#pragma unroll
-      for (int w = 16; w > 0; w >>= 1) l[q] += __shfl_xor_sync(0xffffffffu, l[q], w);
+      const float top = of_query(m, q), sum = of_query(l, q);
       if (q >= queries) continue;
       float* to = reinterpret_cast<float*>(p.out) + (q_row + q) * D + lane * kCols;
 #pragma unroll
-      for (int j = 0; j < kCols; ++j) to[j] = o[q][j] / l[q];
-      if (p.lse && lane == 0) p.lse[q_row + q] = (m[q] + fast_log2(l[q])) * kLn2;
+      for (int j = 0; j < kCols; ++j) to[j] = o[q][j] / sum;
+      if (p.lse && lane == 0) p.lse[q_row + q] = (top + fast_log2(sum)) * kLn2;
     }
   }
 };
