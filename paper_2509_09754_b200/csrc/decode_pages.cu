@@ -18,8 +18,12 @@
 // bf16: S = Q K^T and O += P V by mma.sync m16n8k16 (2 % of the tensor peak at the rate of HBM).  With up to 8 queries
 // the other 8 rows of the A operand are free: they carry what rounding the probabilities to bf16 left over, so the
 // products with V keep 16 bits of every probability at no cost; with 9 to 16 queries a second product does.  More
-// queries per KV head than 16 are taken 16 at a time.  fp32: a lane has a row (or a half or quarter of it) for the
-// logits, and some columns for the product with V; up to 8 queries at a time.
+// queries per KV head than 16 are taken 16 at a time.  fp32: lanes have a share of one or two rows for the logits, and
+// some columns for the product with V; up to 8 queries at a time.
+//
+// Bound by HBM where the heads hold enough (64 x 8 heads of 2048 rows, bf16 of 128: 91 us, 5.8 TB/s where a copy has
+// 6.6; 16 queries a head 105 us; fp32, 32 sequences: 87 us, with 8 queries a head 93), else by the chain of one CTA:
+// counts, page table, rows, joining (5.7 us for one short sequence, 9 where heads are split).
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -160,6 +164,17 @@ __device__ __forceinline__ float top_of(const float2 (*stats)[Q], int q) {
   return top;
 }
 
+// Rows behind a head's last one may hold anything: their probabilities are 0, so must they be.  By one warp.
+template <class S>
+__device__ __forceinline__ void clear_rows(uint32_t tile, int begin, int end) {
+  constexpr int kPieces = S::kRowBytes / 16;
+  for (int i = threadIdx.x & 31; i < (end - begin) * kPieces; i += 32)
+    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(piece_at<S>(tile, begin + i / kPieces, i % kPieces)), "r"(0)
+                 : "memory");
+  fence_async_proxy();  // (before the next copy into this stage)
+  __syncwarp();
+}
+
 // ---- bf16: tensor cores ----------------------------------------------------------------------------
 // Thread (g = lane / 4, t = lane % 4) has query row g, and with 16 queries g + 8 too.
 template <int D, int Q>
@@ -258,13 +273,7 @@ struct TensorWarp {
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[nd][e] *= corr[kRowsOf == 2 ? e >> 1 : 0];
     }
-    if (valid < 16) {  // rows behind the last one may hold anything: their probabilities are 0, so must they be
-      for (int i = lane; i < (16 - valid) * (D / 8); i += 32)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(piece_at<S>(v_tile, r0 + valid + i / (D / 8), i % (D / 8))),
-                     "r"(0) : "memory");
-      fence_async_proxy();  // (before the next copy into this stage)
-      __syncwarp();
-    }
+    if (valid < 16) clear_rows<S>(v_tile, r0 + valid, r0 + 16);
 #pragma unroll
     for (int nd = 0; nd < D / 8; nd += 2) {
       uint32_t b0, b1, b2, b3;
@@ -327,25 +336,27 @@ struct TensorWarp {
 };
 
 // ---- fp32 ------------------------------------------------------------------------------------------
-// A warp has kWarpRows rows of a tile: for the logits lane % kWarpRows is the row and the lanes that share it split
-// its pieces; for the product with V a lane has D / 32 columns.
+// A warp has kWarpRows rows of a tile.  For the logits a lane has kPer of them, lane % kLanes and on, and the lanes that
+// have the same rows split their pieces; two rows, and half as many loads of the queries, wherever there are queries
+// enough for the lanes to split.  For the product with V a lane has D / 32 columns.
 template <int D, int Q>
 struct PlainWarp {
   using S = Shape<D, false, Q>;
-  static constexpr int kRows = S::kWarpRows, kSplit = 32 / kRows, kPieces = D / 4 / kSplit, kCols = D / 32;
+  static constexpr int kRows = S::kWarpRows, kPer = Q * kRows >= 64 ? 2 : 1, kLanes = kRows / kPer;
+  static constexpr int kSplit = 32 / kLanes, kPieces = D / 4 / kSplit, kCols = D / 32;
   static constexpr bool kOwnQueries = kRows == kBoxRows;  // a copy per warp (which may have its own head), or one
   static constexpr int kQueryBytes = Q * D * 4;
   static constexpr int kNext = Q * D / 4 / (kOwnQueries ? 32 : 32 * kConsumers);
   static_assert(kNext >= 1, "a lane has a piece of the queries");
-  // The lanes that share a row split the queries when its logits are summed: each has kOwn of them, from own0() on.
+  // The lanes that share rows split the queries when the logits are summed: each has kOwn of them, from own0() on.
   static constexpr int kOwn = Q / kSplit;
   static_assert(kOwn >= 1 && kOwn * kSplit == Q, "queries of a lane");
   uint4 next[kNext];      // of the queries of the next head
   float m[kOwn], l[kOwn], o[Q][kCols];
-  static __device__ __forceinline__ int own0() { return (threadIdx.x & 31) / kRows * kOwn; }
+  static __device__ __forceinline__ int own0() { return (threadIdx.x & 31) / kLanes * kOwn; }
   // query q's value among those that the lanes have of their own (the same for all rows)
   static __device__ __forceinline__ float of_query(const float (&x)[kOwn], int q) {
-    return __shfl_sync(0xffffffffu, x[q % kOwn], q / kOwn * kRows);
+    return __shfl_sync(0xffffffffu, x[q % kOwn], q / kOwn * kLanes);
   }
 
   __device__ __forceinline__ void fetch(const PageParams& p, size_t q_row, int queries) {
@@ -378,48 +389,64 @@ struct PlainWarp {
 
   __device__ __forceinline__ void tile(uint32_t k_tile, uint32_t v_tile, int r0, int valid, const Logit& logit,
                                        const unsigned char* q_mem, float* probs) {
-    const int lane = threadIdx.x & 31, row = lane % kRows, share = lane / kRows;
+    const int lane = threadIdx.x & 31, row = lane % kLanes, share = lane / kLanes;
     const float* qs = reinterpret_cast<const float*>(q_mem);  // [Q][D]
-    float z[Q] = {};
-#pragma unroll 4
+    // the share's first piece: those of all shares neighbours, and no bank conflicts among eight lanes' pieces of K
+    const int c0 = kLanes == 4 ? (share & 1) * 4 + share / 2 : share;
+    float z[kPer][Q] = {};
+#pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int c = i * kSplit + share;  // (neighbouring pieces: no bank conflicts among the queries')
-      float4 k;
-      asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w)
-                   : "r"(piece_at<S>(k_tile, r0 + row, c)));
+      const int c = i * kSplit + c0;
+      float4 k[kPer];
+#pragma unroll
+      for (int j = 0; j < kPer; ++j)
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(k[j].x), "=f"(k[j].y), "=f"(k[j].z), "=f"(k[j].w)
+                     : "r"(piece_at<S>(k_tile, r0 + row + j * kLanes, c)));
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
         const float4 a = *reinterpret_cast<const float4*>(qs + q * D + 4 * c);
-        z[q] = fmaf(a.x, k.x, fmaf(a.y, k.y, fmaf(a.z, k.z, fmaf(a.w, k.w, z[q]))));
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+          z[j][q] = fmaf(a.x, k[j].x, fmaf(a.y, k[j].y, fmaf(a.z, k[j].z, fmaf(a.w, k[j].w, z[j][q]))));
       }
     }
-    // sums over the lanes of a row, which halve their queries at every step
+    // sums over the lanes that share rows, which halve their queries at every step
     int left = Q;
 #pragma unroll
-    for (int w = 16; w >= kRows; w /= 2) {
+    for (int w = 16; w >= kLanes; w /= 2) {
       left /= 2;
       const bool upper = lane & w;
 #pragma unroll
-      for (int i = 0; i < Q / 2; ++i)
-        if (i < left) {
-          const float away = upper ? z[i] : z[left + i], mine = upper ? z[left + i] : z[i];
-          z[i] = mine + __shfl_xor_sync(0xffffffffu, away, w);
-        }
+      for (int j = 0; j < kPer; ++j)
+#pragma unroll
+        for (int i = 0; i < Q / 2; ++i)
+          if (i < left) {
+            const float away = upper ? z[j][i] : z[j][left + i], mine = upper ? z[j][left + i] : z[j][i];
+            z[j][i] = mine + __shfl_xor_sync(0xffffffffu, away, w);
+          }
     }
     float corr[kOwn];
     bool moved = false;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
-      z[i] = row < valid ? logit.of(z[i]) : -INFINITY;
-      float best = z[i];
+      float best = -INFINITY;
 #pragma unroll
-      for (int w = 1; w < kRows; w *= 2) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, w));
+      for (int j = 0; j < kPer; ++j) {
+        z[j][i] = row + j * kLanes < valid ? logit.of(z[j][i]) : -INFINITY;
+        best = fmaxf(best, z[j][i]);
+      }
+#pragma unroll
+      for (int w = 1; w < kLanes; w *= 2) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, w));
       const float m_new = fmaxf(m[i], best), ref = finite_ref(m_new);
       corr[i] = fast_exp2(m[i] - ref);
       moved |= m_new != m[i];
       m[i] = m_new;
-      z[i] = fast_exp2(z[i] - ref);
-      l[i] = l[i] * corr[i] + z[i];  // a lane's own rows
+      l[i] *= corr[i];
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        z[j][i] = fast_exp2(z[j][i] - ref);
+        l[i] += z[j][i];  // a lane's own rows
+      }
     }
     if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
@@ -430,14 +457,17 @@ struct PlainWarp {
       }
     }
     __syncwarp();  // (the probabilities of the tile before have been read)
-    float* const to = probs + row * Q + own0();
-    if constexpr (kOwn == 4) *reinterpret_cast<float4*>(to) = make_float4(z[0], z[1], z[2], z[3]);
-    else if constexpr (kOwn == 2) *reinterpret_cast<float2*>(to) = make_float2(z[0], z[1]);
-    else to[0] = z[0];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      float* const to = probs + (row + j * kLanes) * Q + own0();
+      if constexpr (kOwn == 4) *reinterpret_cast<float4*>(to) = make_float4(z[j][0], z[j][1], z[j][2], z[j][3]);
+      else if constexpr (kOwn == 2) *reinterpret_cast<float2*>(to) = make_float2(z[j][0], z[j][1]);
+      else to[0] = z[j][0];
+    }
     __syncwarp();
-#pragma unroll 4
+    if (valid < kRows) clear_rows<S>(v_tile, r0 + valid, r0 + kRows);
+#pragma unroll
     for (int r = 0; r < kRows; ++r) {
-      if (r >= valid) break;  // rows behind the last one may hold anything
       float v[kCols];
       if constexpr (kCols == 4)
         asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3])
@@ -464,11 +494,11 @@ struct PlainWarp {
 #pragma unroll
     for (int i = 0; i < kOwn; ++i)
 #pragma unroll
-      for (int w = 1; w < kRows; w *= 2) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
+      for (int w = 1; w < kLanes; w *= 2) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
   }
   __device__ __forceinline__ void leave_stats(float2* ml) {
     sum_rows();
-    if ((threadIdx.x & 31) % kRows == 0)
+    if ((threadIdx.x & 31) % kLanes == 0)
 #pragma unroll
       for (int i = 0; i < kOwn; ++i) ml[own0() + i] = make_float2(m[i], l[i]);
   }
