@@ -23,7 +23,7 @@
 //
 // Bound by HBM where the heads hold enough (64 x 8 heads of 2048 rows, bf16 of 128: 91 us, 5.8 TB/s where a copy has
 // 6.6; 16 queries a head 105 us; fp32, 32 sequences: 87 us, with 8 queries a head 93), else by the chain of one CTA:
-// counts, page table, rows, joining (5.7 us for one short sequence, 9 where heads are split).
+// counts, page table, rows, joining (5.6 us for short sequences, 8 where heads are split).
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -54,7 +54,8 @@ struct Shape {
   static constexpr int kStages = 96 * 1024 / kStageBytes;
   static constexpr int kSmem = kStages * kStageBytes + 1024;     // (aligned to the swizzle's period inside)
   static_assert(kConsumers * Q * D * 4 <= kStageBytes, "the warps' results fit a stage");
-  static constexpr int kSmall = 128 * 1024 / kStageBytes, kLarge = 2 * kSmall;  // tiles of a piece
+  static constexpr int kPieceLog = kStageBytes == 32 * 1024 ? 1 : 2;  // of the tiles of the smallest pieces: 64 KB
+  static_assert(kStageBytes << kPieceLog == 64 * 1024, "smallest pieces");
 };
 
 struct PageParams {
@@ -63,6 +64,7 @@ struct PageParams {
   int heads;               // of the call's layers
   int subs, per_sub;       // a group's queries are taken in `subs` portions of `per_sub`
   int own_queries;         // a warp can have a head of its own
+  int sms;
   const void* q;           // [layers, batch, H_q, d]
   const int* table;
   const int* rows;
@@ -85,24 +87,40 @@ template <class S>
 __device__ __forceinline__ int tiles_of(int len) {
   return (len + S::kTile - 1) / S::kTile;
 }
-// Sums over heads (the host has seen to it that they fit).
+__device__ __forceinline__ int boxes_of(int len) { return (len + kBoxRows - 1) / kBoxRows; }
+// Sums over heads: boxes (the host has seen to it that they fit), and pieces of every size, each twice the one before, two
+// in a word.  More pieces than a call has CTAs need not be told apart, so counts stop where 16 bits hold their sums.
+constexpr int kSizes = 6, kMostPieces = 511;
 struct Counts {
-  int boxes, small, large;  // boxes of 16 rows, pieces of both sizes
+  int boxes;
+  unsigned pieces[kSizes / 2];
   template <class S>
   static __device__ __forceinline__ Counts of(int len) {
-    const int tiles = tiles_of<S>(len);
-    return {(len + kBoxRows - 1) / kBoxRows, (tiles + S::kSmall - 1) / S::kSmall, (tiles + S::kLarge - 1) / S::kLarge};
+    Counts x;
+    x.boxes = boxes_of(len);
+#pragma unroll
+    for (int i = 0; i < kSizes; i += 2)
+      x.pieces[i / 2] = min(pieces_of<S>(len, i), kMostPieces) | min(pieces_of<S>(len, i + 1), kMostPieces) << 16;
+    return x;
   }
-  __device__ __forceinline__ void add(const Counts& y) {
-    boxes += y.boxes;
-    small += y.small;
-    large += y.large;
+  template <class S>
+  static __device__ __forceinline__ int pieces_of(int len, int size) {
+    const int log = S::kPieceLog + size;
+    return (tiles_of<S>(len) + (1 << log) - 1) >> log;
   }
   __device__ __forceinline__ Counts over_warp() const {
-    return {__reduce_add_sync(0xffffffffu, boxes), __reduce_add_sync(0xffffffffu, small),
-            __reduce_add_sync(0xffffffffu, large)};
+    Counts x;
+    x.boxes = __reduce_add_sync(0xffffffffu, boxes);
+#pragma unroll
+    for (int i = 0; i < kSizes / 2; ++i) {
+      const unsigned n = __reduce_add_sync(0xffffffffu, pieces[i]);
+      x.pieces[i] = min(n & 0xffffu, 2u * kMostPieces) | min(n >> 16, 2u * kMostPieces) << 16;
+    }
+    return x;
   }
+  __device__ __forceinline__ int of_size(int i) const { return pieces[i / 2] >> (i % 2 * 16) & 0xffffu; }
 };
+static_assert(32 * 2 * kMostPieces < 65536, "32 heads, or 32 segments");
 __device__ __forceinline__ int head_len(const PageParams& p, int h) {
   return min(max(0, p.rows[p.first_head + h]), p.c.max_pages << p.c.page_shift);
 }
@@ -547,14 +565,18 @@ constexpr int kPieceHeads = 1024;              // heads above which pieces are n
 // How the line is cut (the same in every CTA: it follows from the row counts).
 struct Plan {
   int by_warp;  // 1: whole heads per warp
-  int piece;    // > 0: a portion's tiles in pieces of at most so many, one per CTA
+  int piece;    // i > 0: a portion in pieces of size i - 1, one per CTA
   int parts;    // CTAs that have a part
   int total;    // boxes of all portions (the host has seen to it that 32 bits hold them)
 };
 
-// Heads that are short against a warp's share go whole to warps, which then need not meet.  Else, where few CTAs have
-// work, a portion is cut into pieces of 128 or 256 KB, no more than there are CTAs; and where there is more, the line
-// into equal parts.  (SMs do not get equal shares of the bandwidth: of 64 x 8 heads of 2048 rows the first CTA is through
+// Heads that are short against a warp's share go whole to warps, which then need not meet.  Else, where there are CTAs
+// for it, every CTA gets a piece of one portion: the smallest size that there are CTAs for (for 64 KB: SMs), up to
+// 5/2 of an equal part.  Else the line is cut into equal parts.  These load the SMs better, but most of them end in two
+// heads: two meetings, two partial results.  Pieces / parts, us: 28 x 4 heads of 1024 rows 19.4 (of 256 KB) / 25.0, of
+// 2000 27.8 (512 KB) / 32.6; 8 heads of 30000 rows 29.5 (512 KB) / 33.6, of 60000 47.8 (1 MB) / 49.6; 128 heads of 2400
+// 34.2 (1 MB) / 35.0.  64 KB / 128: 8 heads of 600 rows 7.6 / 8.7, 64 of 150 8.1 / 8.9, 8 of 150 7.8 / 6.8.
+// (SMs do not get equal shares of the bandwidth: of 64 x 8 heads of 2048 rows the first CTA is through
 // after 68 us, the last after 86.  An eighth of the line in small parts for whoever is through did not pay: 105 us against
 // 96, with a twelfth in fewer parts 101; every small part has its own meeting, partial results and joins.)
 template <class S>
@@ -564,15 +586,19 @@ __device__ __forceinline__ Plan plan_of(const PageParams& p, const Counts& all, 
   if (S::kWarpRows == kBoxRows && p.subs == 1 && p.own_queries && (long long)most * grid * kConsumers <= 2ll * all.boxes) {
     plan.by_warp = 1;
     plan.parts = grid;
-  } else if (p.heads <= kPieceHeads && all.small * p.subs <= grid) {
-    plan.piece = S::kSmall;
-    plan.parts = all.small * p.subs;
-  } else if (p.heads <= kPieceHeads && all.large * p.subs <= grid) {
-    plan.piece = S::kLarge;
-    plan.parts = all.large * p.subs;
   } else {
     // (a part is as long as a tile at least, so that a tile begins in it)
     plan.parts = min(grid, max(min(plan.total, 1), plan.total / kBoxesOf<S>));
+    if (p.heads <= kPieceHeads)
+#pragma unroll
+      for (int i = kSizes - 1; i >= 0; --i) {
+        const int n = all.of_size(i) * p.subs;
+        const bool even = i < 2 || ((long long)kBoxesOf<S> * grid << (S::kPieceLog + i)) <= plan.total * 5ll / 2;
+        if (even && n <= min(i == 0 ? p.sms : grid, kMostPieces - 1)) {
+          plan.piece = i + 1;
+          plan.parts = n;
+        }
+      }
   }
   return plan;
 }
@@ -642,14 +668,14 @@ __device__ __forceinline__ int scan_warp(int x) {
   return x;
 }
 
-// The head that unit u of all heads' units is in, and how many units lie before that head; counted(x) picks the units
-// of a head or a segment.  For whole warps.
-template <class S, class Counted>
-__device__ __forceinline__ int2 find_unit(const PageParams& p, const Counts* segs, int seg_heads, int u, Counted counted) {
+// The head that unit u of all heads' units is in, and how many units lie before that head; of_seg(i) and of_len(rows) say
+// how many a segment and a head have.  For whole warps.
+template <class OfSeg, class OfLen>
+__device__ __forceinline__ int2 find_unit(const PageParams& p, int seg_heads, int u, OfSeg of_seg, OfLen of_len) {
   const int lane = threadIdx.x & 31;
   int at = 0, seg = 0;
   for (;; seg += 32) {
-    const int mine = (seg + lane) * seg_heads < p.heads ? counted(segs[seg + lane]) : 0;
+    const int mine = (seg + lane) * seg_heads < p.heads ? of_seg(seg + lane) : 0;
     const int upto = scan_warp(mine);
     const unsigned past = __ballot_sync(0xffffffffu, at + upto > u);
     if (past) {
@@ -662,7 +688,7 @@ __device__ __forceinline__ int2 find_unit(const PageParams& p, const Counts* seg
     if ((seg + 32) * seg_heads >= p.heads) return make_int2(p.heads, at);  // behind the last unit
   }
   for (int h = seg * seg_heads;; h += 32) {
-    const int mine = h + lane < p.heads ? counted(Counts::of<S>(head_len(p, h + lane))) : 0;
+    const int mine = h + lane < p.heads ? of_len(head_len(p, h + lane)) : 0;
     const int upto = scan_warp(mine);
     const unsigned past = __ballot_sync(0xffffffffu, at + upto > u);
     if (past) {
@@ -693,7 +719,7 @@ __device__ __forceinline__ void whole_heads(const PageParams& p, const CUtensorM
     while (n < 32 && next_head < end) {
       // boxes of the next 32 heads, counted on from those in hand
       const int len = next_head + lane < end ? head_len(p, next_head + lane) : 0;
-      const int upto = scan_warp((len + kBoxRows - 1) / kBoxRows - (lane == 0 ? next_row / kBoxRows : 0));
+      const int upto = scan_warp(boxes_of(len) - (lane == 0 ? next_row / kBoxRows : 0));
       const int want = lane - n;    // which of these boxes is this lane's
       int of = 0;                   // the head that it is in: as many heads end before it or with it
 #pragma unroll
@@ -917,14 +943,14 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   // (Little code for few heads: it is fetched anew by every launch.)
   int most = 0, empty = 0;  // boxes of the longest head, heads without rows
   const auto see = [&](int len) {
-    most = max(most, (len + kBoxRows - 1) / kBoxRows);
+    most = max(most, boxes_of(len));
     empty += len == 0;
-    return Counts::of<S>(len);
+    return len;
   };
   if (p.heads <= kPieceHeads) {
     for (int seg = warp; 32 * seg < p.heads; seg += kWarpsAll) {
       const int h = 32 * seg + lane;
-      const Counts sum = (h < p.heads ? see(head_len(p, h)) : Counts{}).over_warp();
+      const Counts sum = Counts::of<S>(h < p.heads ? see(head_len(p, h)) : 0).over_warp();
       if (lane == 0) sh.segs[seg] = sum;
     }
   } else {
@@ -940,11 +966,11 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         }
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          if (len[j] >= 0) mine += see(len[j]).boxes;
+          if (len[j] >= 0) mine += boxes_of(see(len[j]));
           const int h = i + 32 * j;
           if (((h / 32 + 1) & (per_seg - 1)) == 0) {
             const int sum = __reduce_add_sync(0xffffffffu, mine);
-            if (lane == 0 && h - (seg_heads - 32) < p.heads) sh.segs[h / seg_heads] = Counts{sum, 0, 0};
+            if (lane == 0 && h - (seg_heads - 32) < p.heads) sh.segs[h / seg_heads].boxes = sum;
             mine = 0;
           }
         }
@@ -956,7 +982,12 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   if (lane == 0) sh.seen[warp] = make_int2(most, empty);
   __syncthreads();
   Counts all = {};
-  for (int seg = lane; seg * seg_heads < p.heads; seg += 32) all.add(sh.segs[seg]);
+  for (int seg = lane; seg * seg_heads < p.heads; seg += 32) {
+    all.boxes += sh.segs[seg].boxes;
+    if (p.heads <= kPieceHeads)  // (that is one segment a lane)
+#pragma unroll
+      for (int i = 0; i < kSizes / 2; ++i) all.pieces[i] = sh.segs[seg].pieces[i];
+  }
   all = all.over_warp();
 #pragma unroll
   for (int w = 0; w < kWarpsAll; ++w) {
@@ -983,11 +1014,11 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const int cut = part_begin(all.boxes, workers, i + k);
-        const int2 f = find_unit<S>(p, sh.segs, seg_heads, cut, [](const Counts& x) { return x.boxes; });
+        const int2 f = find_unit(p, seg_heads, cut, [&](int i) { return sh.segs[i].boxes; }, boxes_of);
         begin[k] = f.x;
         at[k] = f.y;
         if (f.y < cut && f.x < p.heads) {  // inside a head: the next one
-          at[k] += Counts::of<S>(head_len(p, f.x)).boxes;
+          at[k] += boxes_of(head_len(p, f.x));
           ++begin[k];
         }
       }
@@ -999,17 +1030,16 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   {
     // the piece, or the box, that this CTA's part begins with
     const int unit = plan.piece ? (int)blockIdx.x : part_begin(plan.total, plan.parts, blockIdx.x);
-    const int2 f = find_unit<S>(p, sh.segs, seg_heads, unit, [&](const Counts& x) {
-      return (plan.piece == S::kSmall ? x.small : plan.piece ? x.large : x.boxes) * p.subs;
-    });
-    const int len = head_len(p, f.x), tiles = tiles_of<S>(len);
-    const Counts its = Counts::of<S>(len);
-    const int n = plan.piece == S::kSmall ? its.small : plan.piece ? its.large : its.boxes;
+    const auto of_len = [&](int len) { return plan.piece ? Counts::pieces_of<S>(len, plan.piece - 1) : boxes_of(len); };
+    const int2 f = find_unit(p, seg_heads, unit,
+                             [&](int i) { return (plan.piece ? sh.segs[i].of_size(plan.piece - 1) : sh.segs[i].boxes) * p.subs; },
+                             [&](int len) { return of_len(len) * p.subs; });
+    const int len = head_len(p, f.x), tiles = tiles_of<S>(len), n = of_len(len);
     const int sub = p.subs == 1 ? 0 : (unit - f.y) / n, i = unit - f.y - sub * n;
     if (plan.piece) {
       // (a line of its own, which ends with the piece)
       const int t0 = n == 1 ? 0 : part_begin(tiles, n, i), t1 = n == 1 ? tiles : part_begin(tiles, n, i + 1);
-      part = {f.x, sub, t0, 0, min(its.boxes, t1 * kBoxesOf<S>), unit - i, n};
+      part = {f.x, sub, t0, 0, min(boxes_of(len), t1 * kBoxesOf<S>), unit - i, n};
     } else {
       // the first tile that begins there or behind it: it may be the next portion's
       part = {f.x, sub, (i + kBoxesOf<S> - 1) / kBoxesOf<S>, f.y + sub * n, part_begin(plan.total, plan.parts, blockIdx.x + 1), 0, 0};
@@ -1034,9 +1064,9 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     int done = 0;  // tiles
     bool alive = true;
     for (; at0 < part.end && alive && h < p.heads; ++h, sub = 0) {
-      const int len = head_len(p, h), n = tiles_of<S>(len), boxes_of = (len + kBoxRows - 1) / kBoxRows;
+      const int len = head_len(p, h), n = tiles_of<S>(len), its_boxes = boxes_of(len);
       if (n == 0) continue;
-      for (; sub < p.subs && at0 < part.end && alive; ++sub, t0 = 0, at0 += boxes_of) {
+      for (; sub < p.subs && at0 < part.end && alive; ++sub, t0 = 0, at0 += its_boxes) {
         const int tiles = min(n, (part.end - at0 + kBoxes - 1) / kBoxes) - t0;
         if (tiles <= 0) continue;
         int places = 0;
@@ -1073,9 +1103,9 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     int fetched = -1;  // the head whose queries are on their way
     bool alive = true, begun = false, ended = false;  // others have tiles of the portion that the part begins, ends in
     for (; at0 < part.end && alive && h < p.heads; ++h, sub = 0) {
-      const int len = head_len(p, h), n = tiles_of<S>(len), boxes_of = (len + kBoxRows - 1) / kBoxRows;
+      const int len = head_len(p, h), n = tiles_of<S>(len), its_boxes = boxes_of(len);
       if (n == 0) continue;
-      for (; sub < p.subs && at0 < part.end; ++sub, t0 = 0, at0 += boxes_of) {
+      for (; sub < p.subs && at0 < part.end; ++sub, t0 = 0, at0 += its_boxes) {
         const int tiles = min(n, (part.end - at0 + kBoxesOf<S> - 1) / kBoxesOf<S>) - t0;
         if (tiles <= 0) continue;
         const int queries = min(p.per_sub, c.group - sub * p.per_sub);
@@ -1205,6 +1235,7 @@ lava_status launch(const CUtensorMap& map_k, const CUtensorMap& map_v, PageParam
   const long long most = ((((long long)p.c.max_pages << p.c.page_shift) + S::kTile - 1) / S::kTile) * p.heads * p.subs;
   const int grid = (int)std::min<long long>(most_ctas(), most);
   p.own_queries = WarpOf<D, BF16, Q>::kOwnQueries;
+  p.sms = most_ctas() / kCtasPerSm;
   const cudaError_t e = launch_in_order(kernel, grid, kThreads, S::kSmem, stream, map_k, map_v, p);
   count_launches(1);
   return check_cuda(e, "paged decode attention launch");

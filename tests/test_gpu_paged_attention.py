@@ -359,3 +359,49 @@ def test_rows_far_into_a_large_pool():
     c.first, c.group, c.softcap, c.scale = 0, 4, 0.0, d ** -0.5
     c.flat = [(kh[:n].double().numpy(), vh[:n].double().numpy())]
     c.check(*c.run())
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.float32, 64)])
+@pytest.mark.parametrize("rows", [130, 600, 2500, 9000, 17000, 36000, 80001, 170000])
+def test_few_heads_in_pieces_of_every_size(rows, dtype, d):
+    """Few heads are cut into pieces of 64 KB to 2 MB, as long as there are CTAs for them, or into equal parts.  The heads
+    are long by naming the pages of a small pool again and again; the wanted values come from the rows' multiplicity."""
+    g = torch.Generator().manual_seed(rows)
+    lens = torch.tensor([rows, rows // 2, 1, rows - 7, 0, rows, rows // 3, rows - 64])
+    ps, n_pages, group = 64, 48, 3
+    most = -(-rows // ps)
+    table = torch.randint(0, n_pages, (1, 1, 8, most), generator=g)
+    k, v = (torch.randn((n_pages, ps, d), generator=g).to(dtype).cuda() for _ in range(2))
+    q = torch.randn((1, 1, 8 * group, d), generator=g).to(dtype).cuda()
+    cache = lava.CacheDesc(n_layers=1, batch=1, n_q_heads=8 * group, n_kv_heads=8, head_dim=d, page_rows=ps,
+                           max_pages=most, n_pages=n_pages, dtype=CODE[dtype])
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device="cuda")
+    ws = torch.zeros(lava.lava_cache_workspace_bytes(cache), dtype=torch.uint8, device="cuda")
+    for _ in range(2):
+        lava.lava_decode_attention_pages(cache, 0, q, k, v, table.int().cuda(), lens.int().view(1, 1, 8).cuda(), out, lse, ws)
+    assert lava.lava_poll_status(ws) == 0
+    kd, vd = k.double().view(-1, d), v.double().view(-1, d)
+    for h in range(8):
+        n = int(lens[h])
+        got, got_lse = out[0, 0, h * group: (h + 1) * group].double(), lse[0, 0, h * group: (h + 1) * group].double()
+        if n == 0:
+            assert bool((got == 0).all()) and bool((got_lse == -math.inf).all())
+            continue
+        times = torch.zeros(n_pages * ps, dtype=torch.float64)
+        j = torch.arange(n)
+        times.index_add_(0, table[0, 0, h][j // ps] * ps + j % ps, torch.ones(n, dtype=torch.float64))
+        times = times.cuda()
+        qh = q[0, 0, h * group: (h + 1) * group].double()
+        x = qh @ kd.T / math.sqrt(d)
+        x = torch.where(times > 0, x, -math.inf)
+        p = times * torch.exp(x - x.max(dim=1, keepdim=True).values)
+        want, mag = p @ vd / p.sum(1, keepdim=True), p @ vd.abs() / p.sum(1, keepdim=True)
+        want_lse = x.max(dim=1).values + p.sum(1).log()
+        size = qh.abs() @ kd.abs().T / math.sqrt(d)
+        e = (d * 2.0 ** -23 * size + 2.0 ** -21 * size).max(dim=1, keepdim=True).values
+        # (a warp sums at most a tile's share in one go and adds a sum per tile: no more than n terms in all)
+        tol = (2 * e + 2.0 ** -21 + n * 2.0 ** -23 + (2.0 ** -16 if dtype == torch.bfloat16 else 0.0)) * mag
+        tol += 2.0 ** -8 * (want.abs() + tol) if dtype == torch.bfloat16 else 0.0
+        assert bool(((got - want).abs() <= tol).all()), (h, float(((got - want).abs() / tol).max()))
+        tol = e[:, 0] + 2.0 ** -21 + n * 2.0 ** -23 + 2.0 ** -22 * want_lse.abs()
+        assert bool(((got_lse - want_lse).abs() <= tol).all()), h
