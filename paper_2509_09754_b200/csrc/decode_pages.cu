@@ -571,11 +571,13 @@ struct Plan {
 };
 
 // Heads that are short against a warp's share go whole to warps, which then need not meet.  Else, where there are CTAs
-// for it, every CTA gets a piece of one portion: the smallest size that there are CTAs for (for 64 KB: SMs), up to
-// 5/2 of an equal part.  Else the line is cut into equal parts.  These load the SMs better, but most of them end in two
-// heads: two meetings, two partial results.  Pieces / parts, us: 28 x 4 heads of 1024 rows 19.4 (of 256 KB) / 25.0, of
-// 2000 27.8 (512 KB) / 32.6; 8 heads of 30000 rows 29.5 (512 KB) / 33.6, of 60000 47.8 (1 MB) / 49.6; 128 heads of 2400
-// 34.2 (1 MB) / 35.0.  64 KB / 128: 8 heads of 600 rows 7.6 / 8.7, 64 of 150 8.1 / 8.9, 8 of 150 7.8 / 6.8.
+// for it, every CTA gets a piece of one portion: the whole of it where none is longer than 192 KB, else the smallest
+// size that there are CTAs for (for 64 KB: SMs), up to 256 KB or 5/2 of an equal part.  Else the line is cut into equal
+// parts.  These load the SMs better, but most of them end in two heads: two meetings, two partial results.
+// Pieces / parts, us: 28 x 4 heads of 1024 rows 19.4 (of 256 KB) / 25.0, of 2000 27.8 (512 KB) / 32.6; 8 heads of 30000
+// rows 29.5 (512 KB) / 33.6, of 60000 47.8 (1 MB) / 49.6; 128 heads of 2400 34.2 (1 MB) / 35.0, 256 of 200 12.3 (256 KB)
+// / 14.9.  64 KB / 128: 8 heads of 600 rows 7.6 / 8.7, 64 of 150 8.1 / 8.9.  Whole / pieces: 64 of 80 rows, the longest
+// of 300, 7.3 / 7.9; with heads of up to 256 KB whole 8.6 / 7.8.
 // (SMs do not get equal shares of the bandwidth: of 64 x 8 heads of 2048 rows the first CTA is through
 // after 68 us, the last after 86.  An eighth of the line in small parts for whoever is through did not pay: 105 us against
 // 96, with a twelfth in fewer parts 101; every small part has its own meeting, partial results and joins.)
@@ -589,11 +591,13 @@ __device__ __forceinline__ Plan plan_of(const PageParams& p, const Counts& all, 
   } else {
     // (a part is as long as a tile at least, so that a tile begins in it)
     plan.parts = min(grid, max(min(plan.total, 1), plan.total / kBoxesOf<S>));
+    const bool whole = most * 2 * S::kBoxBytes <= 192 * 1024;
     if (p.heads <= kPieceHeads)
 #pragma unroll
       for (int i = kSizes - 1; i >= 0; --i) {
         const int n = all.of_size(i) * p.subs;
-        const bool even = i < 2 || ((long long)kBoxesOf<S> * grid << (S::kPieceLog + i)) <= plan.total * 5ll / 2;
+        const bool even = i < 3 || ((long long)kBoxesOf<S> * grid << (S::kPieceLog + i)) <= plan.total * 5ll / 2;
+        if (i < 2 && plan.piece == 3 && whole) break;
         if (even && n <= min(i == 0 ? p.sms : grid, kMostPieces - 1)) {
           plan.piece = i + 1;
           plan.parts = n;
