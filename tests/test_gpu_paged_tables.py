@@ -99,6 +99,22 @@ def test_tables_follow_admissions_tokens_and_releases(L, B, H, page_rows, taken)
     assert d.poll() == 0
 
 
+@pytest.mark.parametrize("L,B,H", [(1, 1, 3), (2, 6, 8), (33, 40, 8)])
+def test_heads_of_many_pages(L, B, H):
+    """Heads that take and give back up to 70 pages beside others that take one or none."""
+    g = np.random.default_rng(L)
+    heads = L * B * H
+    d = Device(L, B, H, 16, 75, 80 * min(heads, 60) + 6 * heads, seed=1, taken=heads)
+    counts = np.where(g.random((L, B, H)) < min(1.0, 40 / heads), g.integers(0, 70 * 16, (L, B, H)), g.integers(0, 20, (L, B, H)))
+    assert d.admit(counts)
+    for step in range(3):
+        add = g.integers(0, 40, B)
+        add[g.integers(0, B)] = -1
+        assert d.extend(add.tolist(), 40)
+    assert d.extend([-1] * B, 1)
+    assert d.counters[1] - d.counters[0] == d.n_pages and d.poll() == 0
+
+
 def test_what_does_not_fit_changes_nothing():
     d = Device(1, 2, 2, 16, 3, 6)
     assert d.admit(np.array([[[16, 17], [1, 0]]]))               # 1 + 2 + 1 + 0 pages of 6
