@@ -8,7 +8,7 @@
 // The angle in turns, positions * freqs / (2 pi), is reduced to [-1/2, 1/2] in 64 bits (a position of a million
 // times a frequency of one loses 2^-33 of a turn there, in fp32 1/16 of one) and goes to sincospif in fp32.
 //
-// Bound by reading and writing the vectors once: 6.2 TB/s at 32K tokens, where a copy has 6.6.
+// Bound by reading and writing the vectors once: 6.2 TB/s at 32K tokens, where a copy has 6.6 (1K tokens stay in L2: 5.2 us).
 #include <algorithm>
 
 #include <math.h>
@@ -18,9 +18,9 @@
 namespace lava {
 namespace {
 
-// Threads of a block; heads that a thread has on their way; blocks per SM that the heads are split for.  32K / 1K tokens
-// of 32 + 8 heads (bf16, 128) and 2049 of them in fp32, us: 128 / 2 / 24 108 / 8.0 / 16.4; one head 120 / 8.2 / 17.3,
-// four 130 / 10.8 / 19.8 (256 threads, 16 blocks), two heads with 256 threads 114 / 8.6 / 16.6; 12 blocks 112 / 6.8 / 16.9.
+// Threads of a block; heads that a thread has on their way; blocks per SM that the heads are split for at most.  32K tokens
+// of 32 + 8 heads (bf16, 128) and 2049 of them in fp32, us: 128 / 2 / 24 108 / 16.4; one head 120 / 17.3, four 130 / 19.8
+// (256 threads, 16 blocks), two heads with 256 threads 114 / 16.6; 12 blocks 112 / 16.9.
 constexpr int kThreads = 128;
 constexpr int kAhead = 2;
 constexpr int kBlocks = 24;
@@ -172,9 +172,14 @@ lava_status launch_rotary(const lava_rotary_desc& d, RotaryParams p, cudaStream_
   while (p.tokens_per_block < places && p.tokens_per_block < p.n_tokens) p.tokens_per_block *= 2;
   const long long blocks = (p.n_tokens + p.tokens_per_block - 1) / p.tokens_per_block;
   const int rows = places / p.tokens_per_block;
-  // few tokens: heads over more blocks (each makes the cosines and sines anew)
-  const long long want = (long long)kBlocks * std::max(1, sm_count());
-  const int split = (int)std::max(1ll, std::min((long long)(p.n_heads + rows - 1) / rows, (want + blocks - 1) / blocks));
+  // Few tokens: heads over more blocks, each of which makes the cosines and sines anew; so a thread has two or four heads as
+  // soon as there are blocks enough.  Tokens of 32 + 8 heads, us with one / two / four: 16 2.0 / 2.2 / 2.8; 256 3.5 / 3.1 /
+  // 3.4; 1024 8.0 / 5.9 / 5.2; 4096 18.3 / 18.3 / 17.5.
+  const int sms = std::max(1, sm_count());
+  const long long most = blocks * ((p.n_heads + rows - 1) / rows);
+  const int per = most <= 2 * sms ? 1 : most <= 8 * sms ? 2 : 4;
+  const long long want = (long long)kBlocks * sms, of_heads = (p.n_heads + rows * per - 1) / (rows * per);
+  const int split = (int)std::max(1ll, std::min(of_heads, (want + blocks - 1) / blocks));
   if (blocks > 0x7fffffff) return fail(LAVA_ERR_UNSUPPORTED, "too many tokens");
   const auto kernel = bf16 ? (d.head_dim == 64 ? rotary_kernel<64, true> : rotary_kernel<128, true>)
                            : (d.head_dim == 64 ? rotary_kernel<64, false> : rotary_kernel<128, false>);
