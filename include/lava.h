@@ -510,7 +510,7 @@ LAVA_API lava_status lava_rotary_append(const lava_rotary_desc* rotary, const do
  * for layers first_layer ... first_layer + n_layers - 1 in one call.
  *   q, out      [n_layers, batch, H_q, d], dtype cache->dtype; they must not overlap
  *   lse         float [n_layers, batch, H_q], may be NULL
- *   page_table, head_rows   of the whole cache
+ *   page_table, head_rows   of the whole cache; they must not change while the call runs
  *   workspace   lava_cache_workspace_bytes(cache) bytes, zeroed once
  * The heads of a call times max_pages * page_rows stay below 2^35 (times the portions of 16 queries, 8 with
  * fp32, that a group has).  A head without rows gives zeros and lse = -infinity.  Sums, maxima and the output before its last

@@ -691,7 +691,7 @@ __device__ __forceinline__ int2 find_unit(const PageParams& p, int seg_heads, in
     at += __shfl_sync(0xffffffffu, upto, 31);
     if ((seg + 32) * seg_heads >= p.heads) return make_int2(p.heads, at);  // behind the last unit
   }
-  for (int h = seg * seg_heads;; h += 32) {
+  for (int h = seg * seg_heads; h < p.heads; h += 32) {
     const int mine = h + lane < p.heads ? of_len(head_len(p, h + lane)) : 0;
     const int upto = scan_warp(mine);
     const unsigned past = __ballot_sync(0xffffffffu, at + upto > u);
@@ -701,6 +701,7 @@ __device__ __forceinline__ int2 find_unit(const PageParams& p, int seg_heads, in
     }
     at += __shfl_sync(0xffffffffu, upto, 31);
   }
+  return make_int2(p.heads, at);
 }
 
 // One warp's heads [h, end) of `boxes` boxes in all, alone: it fetches its own boxes, a place in every stage.  32 boxes
@@ -1038,6 +1039,7 @@ decode_pages_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     const int2 f = find_unit(p, seg_heads, unit,
                              [&](int i) { return (plan.piece ? sh.segs[i].of_size(plan.piece - 1) : sh.segs[i].boxes) * p.subs; },
                              [&](int len) { return of_len(len) * p.subs; });
+    if (f.x >= p.heads) return;  // (only where row counts have changed since they were counted, which no caller may do)
     const int len = head_len(p, f.x), tiles = tiles_of<S>(len), n = of_len(len);
     const int sub = p.subs == 1 ? 0 : (unit - f.y) / n, i = unit - f.y - sub * n;
     if (plan.piece) {

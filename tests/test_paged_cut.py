@@ -68,3 +68,44 @@ def test_parts_of_a_line():
             assert begins[0] == 0 and begins[-1] == total
             for i in range(parts):
                 assert all(part_of(total, parts, u) == i for u in range(begins[i], begins[i + 1]))
+
+
+def find_unit(units, seg_heads, u):
+    """The head that unit u is in and the units before it, searched in segments of heads, then in 32 heads at a time; reads
+    of heads that are not there fail."""
+    at, seg, heads = 0, 0, len(units)
+    while True:
+        sums = [sum(units[i * seg_heads: (i + 1) * seg_heads]) if i * seg_heads < heads else 0 for i in range(seg, seg + 32)]
+        upto = [sum(sums[: i + 1]) for i in range(32)]
+        past = [i for i in range(32) if at + upto[i] > u]
+        if past:
+            at += upto[past[0]] - sums[past[0]]
+            seg += past[0]
+            break
+        at += upto[31]
+        if (seg + 32) * seg_heads >= heads:
+            return heads, at
+        seg += 32
+    h = seg * seg_heads
+    while h < heads:
+        mine = [units[h + i] if h + i < heads else 0 for i in range(32)]
+        upto = [sum(mine[: i + 1]) for i in range(32)]
+        past = [i for i in range(32) if at + upto[i] > u]
+        if past:
+            return h + past[0], at + upto[past[0]] - mine[past[0]]
+        at += upto[31]
+        h += 32
+    return heads, at
+
+
+@pytest.mark.parametrize("heads,seg_heads", [(1, 32), (4, 32), (32, 32), (33, 32), (1024, 32), (1025, 32), (3000, 64)])
+def test_the_search_for_a_unit_ends_and_finds_it(heads, seg_heads):
+    rng = random.Random(heads)
+    for units in ([0] * heads, [1] * heads, [rng.choice([0, 0, 1, 5]) for _ in range(heads)]):
+        total = sum(units)
+        for u in {0, total // 3, total - 1, total, total + 7}:
+            h, before = find_unit(units, seg_heads, u)
+            if 0 <= u < total:
+                assert before <= u < before + units[h] and before == sum(units[:h])
+            elif u >= total:
+                assert (h, before) == (heads, total)
