@@ -193,6 +193,9 @@ class PagedCache:
         self.counters = torch.tensor([0, desc.n_pages], dtype=torch.int64, device=device)
         self.workspace = torch.zeros(need, dtype=torch.uint8, device=device)
         self.slots = None  # of the last extend
+        # by number of rows: a captured extend keeps their address, and a stream may be behind the one that calls next, so
+        # none is given up while the cache lives
+        self._slots = {}
 
     def free_page_count(self) -> int:
         """Pages that are free; waits for the device."""
@@ -223,14 +226,15 @@ class PagedCache:
 
     def extend(self, add, max_add: int = 1, stream=None) -> torch.Tensor:
         """Room for add[b] new rows in every head of sequence b, -1 releases it; the rows' places (in memory of the
-        cache's own, which `append` reads and the next call writes)."""
+        cache's own, which `append` reads and the next call with the same max_add writes)."""
         d = self.desc
-        shape = (d.n_layers, d.batch, max_add, d.n_kv_heads)
-        if self.slots is None or self.slots.shape != shape:
-            self.slots = _empty(shape, torch.int32, self.head_rows.device, stream)
-        lava_page_extend(d, add, self.head_rows, self.page_table, self.free_pages, self.counters, self.slots,
+        slots = self._slots.get(max_add)
+        if slots is None:
+            slots = _empty((d.n_layers, d.batch, max_add, d.n_kv_heads), torch.int32, self.head_rows.device, stream)
+        lava_page_extend(d, add, self.head_rows, self.page_table, self.free_pages, self.counters, slots,
                          self.workspace, stream=stream)
-        return self.slots
+        self.slots = self._slots[max_add] = slots
+        return slots
 
     def append(self, rotary: RotaryDesc, freqs, layer: int, positions, q, k, v, q_out=None, stream=None):
         """Turned queries of the new tokens; their turned keys and their values go where `extend` made room."""
