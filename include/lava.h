@@ -202,6 +202,8 @@ LAVA_API lava_status lava_score_layer_static(const lava_layer_desc* desc, const 
  * Rule: shares proportional to e_l are rounded by largest remainder (ties to the lower layer);
  * layers outside [floor, cap] are clamped one side at a time (the side with the larger total
  * violation, the floor side on a tie) and the rest is re-shared among the remaining layers.
+ * A total outside [L*floor, L*cap] is clamped to it first: a packed cache has room for the larger of
+ * total_budget[b] and L*floor rows of every sequence.
  * n_layers <= 256, batch <= 1024. */
 LAVA_API lava_status lava_layer_budgets(int32_t n_layers, int32_t batch, const double* entropy,
                                const int64_t* total_budget, const int64_t* floor_per_layer,

@@ -405,7 +405,7 @@ class EvictionPlan:
     layer_row_offset: torch.Tensor   # int64 [L*batch + 1]
     keep_idx: torch.Tensor           # int32 [L, total_scores]
     head_offsets: torch.Tensor       # int32 [L, batch, H_kv + 1]
-    k_out: torch.Tensor              # [sum of budgets, d]
+    k_out: torch.Tensor              # [sum of budgets, each at least n_layers * H_kv * window, d]
     v_out: torch.Tensor
     workspace: torch.Tensor          # uint8
 
@@ -417,7 +417,8 @@ class EvictionPlan:
         tb = torch.tensor([int(x) for x in total_budget], **i64)
         floor = torch.tensor([hkv * desc.window] * batch, **i64)
         cap = torch.tensor([hkv * int(n) for n in seq_lens], **i64)
-        rows = int(sum(int(x) for x in total_budget))
+        # (budgets below a window per head and layer are raised to it)
+        rows = sum(max(int(x), n_layers * hkv * desc.window) for x in total_budget)
         ts = desc.total_scores
         ws = torch.zeros(lava_workspace_bytes(desc, n_layers), dtype=torch.uint8, device=device)
         return EvictionPlan(
