@@ -220,7 +220,9 @@ LAVA_API lava_status lava_layer_budgets(int32_t n_layers, int32_t batch, const d
  *                 first (layer_budget[b] - H_kv*w) entries of the segment are written
  *   head_offsets  out int32 [batch, H_kv+1]: exclusive scan of rows per head (kept prefix
  *                 rows + w window rows); head_offsets[b][H_kv] == min(layer_budget[b], H_kv*n_b)
- * The per-head differences of head_offsets are the dynamic head budgets. */
+ * The per-head differences of head_offsets are the dynamic head budgets.  Where a sequence of the
+ * batch is shorter than the window (LAVA_DEV_SHORT_SEQUENCE) nothing is selected: keep_idx is left
+ * as it is, and head_offsets are zeros. */
 LAVA_API lava_status lava_select_topk(const lava_layer_desc* desc, const float* scores,
                              const int64_t* layer_budget, int32_t* keep_idx,
                              int32_t* head_offsets, void* workspace, size_t workspace_bytes,
@@ -414,8 +416,7 @@ LAVA_API size_t lava_cache_workspace_bytes(const lava_cache_desc* cache);
  * suffice or a count does not fit.
  *   lava_page_admit   the selection of new prompts: sequences first_seq ... first_seq + n_seqs - 1
  *       of the cache get head_offsets[l][s][g+1] - head_offsets[l][s][g] more rows (head_offsets
- *       [n_layers, n_seqs, H_kv+1] as written by lava_select_topk_layers.  That leaves them as they were
- *       where a sequence is shorter than the window: zeros there before it admit nothing then).
+ *       [n_layers, n_seqs, H_kv+1] as written by lava_select_topk_layers)
  *       first_row   out int32 [n_layers, n_seqs, H_kv]: where a head's new rows start
  *   lava_page_extend  a decode step: every head of sequence b gets add[b] more rows (device int32
  *       [batch], 0 ... max_add), or, where add[b] < 0, gives all its pages back and holds no rows.

@@ -663,9 +663,14 @@ select_topk_kernel(Geom g, const float* scores, const long long* layer_budget, i
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   }
   if (ADOPT && beside) fence_gpu();
-  if (!batch_has_short_sequence(g))  // every CTA of the cluster sees the same lengths
-    select_problem<LIST, ADOPT>(sh, dyn, g, blockIdx.x / cg::this_cluster().num_blocks(), scores, layer_budget,
-                                keep_idx, head_offsets, io);
+  const int cl = blockIdx.x / cg::this_cluster().num_blocks();
+  if (!batch_has_short_sequence(g)) {  // every CTA of the cluster sees the same lengths
+    select_problem<LIST, ADOPT>(sh, dyn, g, cl, scores, layer_budget, keep_idx, head_offsets, io);
+  } else if (!LIST && !ADOPT) {
+    // nothing is selected, and the array may still have the rows of a batch before (a cascade's is its own)
+    const int prob = (g.flags & LAVA_FLAG_PER_HEAD_TOPK) ? cl / g.n_kv_heads : cl;
+    for (int i = threadIdx.x; i <= g.n_kv_heads; i += kThreads) head_offsets[(size_t)prob * (g.n_kv_heads + 1) + i] = 0;
+  }
   if (ADOPT && beside) in_stream_order();
 }
 

@@ -167,10 +167,14 @@ __global__ void __launch_bounds__(1024)
 shard_emit_kernel(Geom g, const float* scores, const ShardState* state, const uint2* counts,
                   const long long* ties_before_rank, int* keep_idx, int* head_offsets,
                   long long* rows_out) {
-  if (batch_has_short_sequence(g)) return;  // the score layout has no room for such a batch
+  const int prob = blockIdx.y, layer = prob / g.batch, head = blockIdx.x;
+  if (batch_has_short_sequence(g)) {  // the score layout has no room for such a batch: no rows
+    if (threadIdx.x <= 1) head_offsets[(size_t)prob * (g.n_kv_heads + 1) + head + threadIdx.x] = 0;
+    if (rows_out && head == 0 && threadIdx.x == 0) rows_out[prob] = 0;
+    return;
+  }
   __shared__ unsigned wsum[32];
   __shared__ unsigned run_keep, run_eq;
-  const int prob = blockIdx.y, layer = prob / g.batch, head = blockIdx.x;
   const SeqInfo s = seq_info(g, prob - layer * g.batch);
   const int win = min(g.window, s.n);
   const ShardState st = state[prob];

@@ -207,8 +207,10 @@ class PagedCache:
         return lava_poll_status(self.workspace, stream)
 
     def admit(self, plan: EvictionPlan, k, v, first_seq: int = 0, stream=None) -> None:
-        """The selection of a plan (its keep_idx and head_offsets) as sequences first_seq ... of the cache: pages, and
-        the kept rows of k and v [n_layers, H_kv, total_tokens, d] in them, behind what the sequences hold."""
+        """The selection of a plan (its keep_idx and head_offsets, after evict_scores or evict_model) as sequences
+        first_seq ... of the cache: pages, and the kept rows of k and v [n_layers, H_kv, total_tokens, d] in them, behind
+        what the sequences hold.  Of a batch with a sequence shorter than the window nothing is selected (the plan's status
+        word says so), and nothing enters."""
         d = self.desc
         first_row = _empty((d.n_layers, plan.desc.batch, d.n_kv_heads), torch.int32, self.head_rows.device, stream)
         lava_page_admit(d, first_seq, plan.head_offsets, self.head_rows, self.page_table, self.free_pages,
@@ -217,10 +219,7 @@ class PagedCache:
                               plan.head_offsets, first_row, self.page_table, self.k_pages, self.v_pages, stream)
 
     def evict(self, plan: EvictionPlan, q_win, k, v, first_seq: int = 0, mode: int = 0, stream=None) -> None:
-        """evict_model with the kept rows in the pages of this cache instead of the plan's packed cache.  A batch with a
-        sequence shorter than the window is left alone as there (the plan's status word says so): nothing enters."""
-        with torch.cuda.stream(stream):
-            plan.head_offsets.zero_()  # (the selection of such a batch writes none)
+        """evict_model with the kept rows in the pages of this cache instead of the plan's packed cache."""
         evict_scores(plan, q_win, k, v, mode, stream)
         self.admit(plan, k, v, first_seq, stream)
 
