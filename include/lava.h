@@ -446,6 +446,14 @@ LAVA_API lava_status lava_compact_kv_pages(const lava_layer_desc* desc, const la
                                            const int32_t* keep_idx, const int32_t* head_offsets,
                                            const int32_t* first_row, const int32_t* page_table,
                                            void* k_pages, void* v_pages, void* stream);
+/* What lava_compact_kv_pages refuses, without any device work: asked before lava_page_admit it keeps a
+ * refused compaction from leaving pages behind that no row was written to. */
+LAVA_API lava_status lava_check_compact_kv_pages(const lava_layer_desc* desc, const lava_cache_desc* cache,
+                                                 int32_t first_seq, const void* k, const void* v,
+                                                 int64_t k_layer_stride, int64_t v_layer_stride,
+                                                 const int32_t* keep_idx, const int32_t* head_offsets,
+                                                 const int32_t* first_row, const int32_t* page_table,
+                                                 const void* k_pages, const void* v_pages);
 
 /* Rotary positions.  Pair i of a vector's leading rotary_dim elements turns by the angle
  * positions[token] * freqs[i]:  (a, b) -> scale * (a cos - b sin, b cos + a sin); the other elements

@@ -21,6 +21,6 @@ from .binding import (  # noqa: F401
 from .paged import (  # noqa: F401
     LAVA_ROTARY_PLAIN, LAVA_ROTARY_LINEAR, LAVA_ROTARY_BASE, LAVA_ROTARY_BANDS, LAVA_ROTARY_RAMP,
     LAVA_DEV_PAGES_EXHAUSTED, LAVA_DEV_BAD_ROWS, CacheDesc, RotaryDesc, PagedCache,
-    lava_cache_workspace_bytes, lava_page_admit, lava_page_extend, lava_compact_kv_pages, lava_rotary_freqs,
-    lava_rotary, lava_rotary_append, lava_decode_attention_pages,
+    lava_cache_workspace_bytes, lava_page_admit, lava_page_extend, lava_compact_kv_pages, lava_check_compact_kv_pages,
+    lava_rotary_freqs, lava_rotary, lava_rotary_append, lava_decode_attention_pages,
 )

@@ -150,11 +150,13 @@ def load_library():
     lib.lava_page_admit.argtypes = [cp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.lava_page_extend.argtypes = [cp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.lava_compact_kv_pages.argtypes = [dp, cp, i32, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp]
+    lib.lava_check_compact_kv_pages.argtypes = [dp, cp, i32, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp]
     lib.lava_rotary_freqs.argtypes = [i32, i32, f64, f64, f64, f64, f64, vp, vp]
     lib.lava_rotary.argtypes = [rp, vp, i64, vp] + 2 * [vp, i32, i64, i64, vp, i64, i64] + [vp]
     lib.lava_rotary_append.argtypes = [rp, vp, cp, i64, vp, vp, i64, i64, vp, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp]
     lib.lava_decode_attention_pages.argtypes = [cp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
-    for name in ("lava_page_admit", "lava_page_extend", "lava_compact_kv_pages", "lava_rotary_freqs",
+    for name in ("lava_page_admit", "lava_page_extend", "lava_compact_kv_pages",
+                 "lava_check_compact_kv_pages", "lava_rotary_freqs",
                  "lava_rotary", "lava_rotary_append", "lava_decode_attention_pages"):
         getattr(lib, name).restype = i32
     for name in ("lava_poll_status", "lava_wo_norm", "lava_score_layer", "lava_score_layers",

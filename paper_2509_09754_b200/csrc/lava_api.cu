@@ -281,6 +281,31 @@ lava_status score_layers_in(const lava_layer_desc* desc, int n_layers, const voi
                                     nullptr, nullptr, nullptr, st);
 }
 
+static lava_status check_compact_pages(const lava_layer_desc* desc, const lava_cache_desc* cache, int32_t first_seq,
+                                       const void* k, const void* v, int64_t k_layer_stride, int64_t v_layer_stride,
+                                       const int32_t* keep_idx, const int32_t* head_offsets, const int32_t* first_row,
+                                       const int32_t* page_table, const void* k_pages, const void* v_pages, Geom* g,
+                                       Cache* c) {
+  lava_status rc = make_geom(desc, g);
+  if (rc == LAVA_OK) rc = make_cache(cache, c);
+  if (rc != LAVA_OK) return rc;
+  if (g->n_kv_heads != c->n_kv_heads || g->head_dim != c->head_dim || g->dtype != c->dtype)
+    return fail(LAVA_ERR_INVALID_ARG, "desc and cache differ in n_kv_heads, head_dim or dtype");
+  if (first_seq < 0 || first_seq > c->batch - g->batch)
+    return fail(LAVA_ERR_INVALID_ARG, "sequences %d ... %lld are not all in a cache of %d", first_seq,
+                (long long)first_seq + g->batch - 1, c->batch);
+  if (!k || !v || !head_offsets || !first_row || !page_table || !k_pages || !v_pages ||
+      (!keep_idx && g->total_scores > 0))
+    return fail(LAVA_ERR_INVALID_ARG, "NULL argument");
+  if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages))
+    return fail(LAVA_ERR_INVALID_ARG, "k, v, k_pages and v_pages must be 16-byte aligned");
+  if (k_layer_stride < 0 || v_layer_stride < 0 || k_layer_stride % 8 != 0 || v_layer_stride % 8 != 0)
+    return fail(LAVA_ERR_INVALID_ARG, "strides must be non-negative multiples of 8 elements");
+  if ((long long)c->n_layers * g->batch > 65535)
+    return fail(LAVA_ERR_UNSUPPORTED, "n_layers*batch must be <= 65535");
+  return LAVA_OK;
+}
+
 }  // namespace lava
 
 using namespace lava;
@@ -452,6 +477,17 @@ lava_status lava_compact_kv_layers(const lava_layer_desc* desc, int32_t n_layers
                         (const long long*)layer_row_offset, k_out, v_out, (cudaStream_t)stream);
 }
 
+lava_status lava_check_compact_kv_pages(const lava_layer_desc* desc, const lava_cache_desc* cache,
+                                        int32_t first_seq, const void* k, const void* v, int64_t k_layer_stride,
+                                        int64_t v_layer_stride, const int32_t* keep_idx,
+                                        const int32_t* head_offsets, const int32_t* first_row,
+                                        const int32_t* page_table, const void* k_pages, const void* v_pages) {
+  Geom g;
+  Cache c;
+  return check_compact_pages(desc, cache, first_seq, k, v, k_layer_stride, v_layer_stride, keep_idx, head_offsets,
+                             first_row, page_table, k_pages, v_pages, &g, &c);
+}
+
 lava_status lava_compact_kv_pages(const lava_layer_desc* desc, const lava_cache_desc* cache,
                                   int32_t first_seq, const void* k, const void* v, int64_t k_layer_stride,
                                   int64_t v_layer_stride, const int32_t* keep_idx,
@@ -459,23 +495,9 @@ lava_status lava_compact_kv_pages(const lava_layer_desc* desc, const lava_cache_
                                   const int32_t* page_table, void* k_pages, void* v_pages, void* stream) {
   Geom g;
   Cache c;
-  lava_status rc = make_geom(desc, &g);
-  if (rc == LAVA_OK) rc = make_cache(cache, &c);
+  const lava_status rc = check_compact_pages(desc, cache, first_seq, k, v, k_layer_stride, v_layer_stride, keep_idx,
+                                             head_offsets, first_row, page_table, k_pages, v_pages, &g, &c);
   if (rc != LAVA_OK) return rc;
-  if (g.n_kv_heads != c.n_kv_heads || g.head_dim != c.head_dim || g.dtype != c.dtype)
-    return fail(LAVA_ERR_INVALID_ARG, "desc and cache differ in n_kv_heads, head_dim or dtype");
-  if (first_seq < 0 || first_seq > c.batch - g.batch)
-    return fail(LAVA_ERR_INVALID_ARG, "sequences %d ... %lld are not all in a cache of %d", first_seq,
-                (long long)first_seq + g.batch - 1, c.batch);
-  if (!k || !v || !head_offsets || !first_row || !page_table || !k_pages || !v_pages ||
-      (!keep_idx && g.total_scores > 0))
-    return fail(LAVA_ERR_INVALID_ARG, "NULL argument");
-  if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages))
-    return fail(LAVA_ERR_INVALID_ARG, "k, v, k_pages and v_pages must be 16-byte aligned");
-  if (k_layer_stride < 0 || v_layer_stride < 0 || k_layer_stride % 8 != 0 || v_layer_stride % 8 != 0)
-    return fail(LAVA_ERR_INVALID_ARG, "strides must be non-negative multiples of 8 elements");
-  if ((long long)c.n_layers * g.batch > 65535)
-    return fail(LAVA_ERR_UNSUPPORTED, "n_layers*batch must be <= 65535");
   return launch_compact_pages(g, c, first_seq, k, v, k_layer_stride, v_layer_stride, keep_idx, head_offsets,
                               first_row, page_table, k_pages, v_pages, (cudaStream_t)stream);
 }

@@ -224,7 +224,9 @@ PyObject* page_extend(PyObject* const* args, Py_ssize_t n) {
   });
 }
 
-PyObject* compact_kv_pages(PyObject* const* args, Py_ssize_t n) {
+// The compaction, or what it refuses alone.
+template <bool CHECK>
+PyObject* compact_pages(PyObject* const* args, Py_ssize_t n) {
   Call c(args, n, 14);
   const auto* layer = c.desc<lava_layer_desc>();
   const auto* d = c.desc<lava_cache_desc>();
@@ -257,10 +259,14 @@ PyObject* compact_kv_pages(PyObject* const* args, Py_ssize_t n) {
   if (!c.ok()) return nullptr;
   const void *k = kv[0]->data_ptr(), *v = kv[1]->data_ptr();
   return finish([&] {
-    return lava_compact_kv_pages(layer, d, first_seq, k, v, k_ls, v_ls, keep, hoff, first_row, table, k_pages,
-                                 v_pages, stream);
+    return CHECK ? lava_check_compact_kv_pages(layer, d, first_seq, k, v, k_ls, v_ls, keep, hoff, first_row, table, k_pages,
+                                               v_pages)
+                 : lava_compact_kv_pages(layer, d, first_seq, k, v, k_ls, v_ls, keep, hoff, first_row, table, k_pages,
+                                         v_pages, stream);
   });
 }
+PyObject* compact_kv_pages(PyObject* const* args, Py_ssize_t n) { return compact_pages<false>(args, n); }
+PyObject* check_compact_kv_pages(PyObject* const* args, Py_ssize_t n) { return compact_pages<true>(args, n); }
 
 const double* frequencies(Call& c, const lava_rotary_desc* r) {
   if (r->rotary_dim == 0 && c.none()) return nullptr;
@@ -383,6 +389,7 @@ PyObject* set_error(PyObject*, PyObject* type) {
 
 #define LAVA_METHOD(name) {#name, (PyCFunction)(void*)guarded<name>, METH_FASTCALL, ""}
 PyMethodDef g_methods[] = {LAVA_METHOD(page_admit),     LAVA_METHOD(page_extend), LAVA_METHOD(compact_kv_pages),
+                           LAVA_METHOD(check_compact_kv_pages),
                            LAVA_METHOD(rotary),         LAVA_METHOD(rotary_append), LAVA_METHOD(decode_attention_pages),
                            {"set_error", set_error, METH_O, "the class that refusals raise"},
                            {nullptr, nullptr, 0, nullptr}};

@@ -133,6 +133,15 @@ def lava_compact_kv_pages(desc: LayerDesc, cache: CacheDesc, first_seq, k, v, k_
         first_row, page_table, k_pages, v_pages, _handle(stream))
 
 
+def lava_check_compact_kv_pages(desc: LayerDesc, cache: CacheDesc, first_seq, k, v, k_layer_stride, v_layer_stride,
+                                keep_idx, head_offsets, first_row, page_table, k_pages, v_pages) -> None:
+    """Raises what lava_compact_kv_pages would, and does nothing."""
+    layer = desc._for_call()
+    (_CALLS or load_paged_calls()).check_compact_kv_pages(
+        ctypes.addressof(layer), cache._at, first_seq, k, v, k_layer_stride, v_layer_stride, keep_idx, head_offsets,
+        first_row, page_table, k_pages, v_pages, None)
+
+
 # ----------------------------------------------------------------------------- rotary positions
 def lava_rotary_freqs(rotary_dim: int, base: float = 10000.0, kind: int = LAVA_ROTARY_PLAIN, factor: float = 1.0,
                       original_length: float = 8192.0, low: float = 1.0, high: float = 4.0):
@@ -213,10 +222,12 @@ class PagedCache:
         word says so), and nothing enters."""
         d = self.desc
         first_row = _empty((d.n_layers, plan.desc.batch, d.n_kv_heads), torch.int32, self.head_rows.device, stream)
+        rows = (plan.desc, d, first_seq, k, v, k.stride(0), v.stride(0), plan.keep_idx, plan.head_offsets, first_row,
+                self.page_table, self.k_pages, self.v_pages)
+        lava_check_compact_kv_pages(*rows)  # (a refusal after the next call would leave pages without their rows)
         lava_page_admit(d, first_seq, plan.head_offsets, self.head_rows, self.page_table, self.free_pages,
                         self.counters, first_row, self.workspace, stream=stream)
-        lava_compact_kv_pages(plan.desc, d, first_seq, k, v, k.stride(0), v.stride(0), plan.keep_idx,
-                              plan.head_offsets, first_row, self.page_table, self.k_pages, self.v_pages, stream)
+        lava_compact_kv_pages(*rows, stream)
 
     def evict(self, plan: EvictionPlan, q_win, k, v, first_seq: int = 0, mode: int = 0, stream=None) -> None:
         """evict_model with the kept rows in the pages of this cache instead of the plan's packed cache."""
