@@ -1,10 +1,14 @@
-"""Builds liblava.so (sm_100a) with nvcc and the paged cache's calls from Python with g++, both in-tree.
-`python -m paper_2509_09754_b200.build`."""
+"""Builds liblava.so (sm_100a) with nvcc and, where torch, Python's headers and g++ are there, the paged cache's calls from
+Python, both in-tree.  `python -m paper_2509_09754_b200.build`; the library alone, for use from C, needs neither:
+`python paper_2509_09754_b200/build.py`."""
 from __future__ import annotations
 
+import importlib.util
 import os
+import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -36,7 +40,8 @@ def _stale(out: str, deps) -> bool:
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu under csrc/ into one shared library; returns its path."""
+    """Compile every .cu under csrc/ into one shared library, and the module of calls where its tools are there; returns
+    the library's path."""
     os.makedirs(LIB_DIR, exist_ok=True)
     obj_dir = os.path.join(PKG, "_build")
     os.makedirs(obj_dir, exist_ok=True)
@@ -58,20 +63,32 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         cmd = [_nvcc(), "-shared", "-o", LIB_PATH] + objs + ["-gencode",
                "arch=compute_100a,code=sm_100a", "-cudart", "static"]
         subprocess.run(cmd, check=True)
-    build_calls(force, verbose)
+    missing = missing_for_calls()
+    if missing:
+        print("%s: not there; the library is built, the paged cache's calls from Python are not" % ", ".join(missing),
+              file=sys.stderr)
+    else:
+        build_calls(force, verbose)
     return LIB_PATH
+
+
+def missing_for_calls() -> list:
+    """What build_calls() needs and does not find."""
+    there = {"torch": importlib.util.find_spec("torch"), "g++": shutil.which("g++"),
+             "Python.h": os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h"))}
+    return [name for name, x in there.items() if not x]
 
 
 def build_calls(force: bool = False, verbose: bool = False) -> str:
     """Compile csrc/paged_calls.cpp into the module that paged.py loads; returns its path."""
-    import sysconfig
     import torch
     src, header = os.path.join(CSRC, "paged_calls.cpp"), os.path.join(ROOT, "include", "lava.h")
     home = os.path.dirname(torch.__file__)
     if force or _stale(CALLS_PATH, [src, header, os.path.join(home, "version.py")]):
         cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
         cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
-               "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+               "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+               '-DLAVA_TORCH_VERSION="%s"' % torch.__version__]
         for inc in (os.path.join(ROOT, "include"), os.path.join(home, "include"),
                     os.path.join(home, "include", "torch", "csrc", "api", "include"),
                     sysconfig.get_paths()["include"], os.path.join(cuda, "include")):

@@ -397,4 +397,9 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_paged_calls", nullptr, -1, g_me
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__paged_calls() { return PyModule_Create(&g_module); }
+PyMODINIT_FUNC PyInit__paged_calls() {
+  PyObject* m = PyModule_Create(&g_module);
+  // tensors are looked into as this torch lays them out: the loader compares
+  if (m && PyModule_AddStringConstant(m, "torch_version", LAVA_TORCH_VERSION) < 0) Py_CLEAR(m);
+  return m;
+}

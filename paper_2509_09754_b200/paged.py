@@ -25,7 +25,7 @@ _CALLS = None
 
 
 def load_paged_calls():
-    """Load the native module; raises if it has not been built (there is no fallback path)."""
+    """Load the native module; raises if it has not been built, or for another torch (there is no fallback path)."""
     global _CALLS
     if _CALLS is None:
         load_library()
@@ -33,8 +33,15 @@ def load_paged_calls():
         if not os.path.exists(path):
             raise RuntimeError("%s is missing: build it with `python -m paper_2509_09754_b200.build`" % path)
         loader = importlib.machinery.ExtensionFileLoader("_paged_calls", path)
-        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_paged_calls", loader))
-        loader.exec_module(module)
+        try:
+            module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_paged_calls", loader))
+            loader.exec_module(module)
+            built = "torch " + module.torch_version
+        except (ImportError, AttributeError) as e:
+            built = "another torch (%s)" % e
+        if built != "torch %s" % torch.__version__:
+            raise RuntimeError("%s was built for %s, this is torch %s: build it again with "
+                               "`python -m paper_2509_09754_b200.build --force`" % (path, built, torch.__version__))
         module.set_error(LavaError)
         _CALLS = module
     return _CALLS
