@@ -591,7 +591,7 @@ __device__ __forceinline__ Plan plan_of(const PageParams& p, const Counts& all, 
   } else {
     // (a part is as long as a tile at least, so that a tile begins in it)
     plan.parts = min(grid, max(min(plan.total, 1), plan.total / kBoxesOf<S>));
-    const bool whole = most * 2 * S::kBoxBytes <= 192 * 1024;
+    const bool whole = most <= 192 * 1024 / (2 * S::kBoxBytes);  // (bytes of a long head need not fit 32 bits)
     if (p.heads <= kPieceHeads)
 #pragma unroll
       for (int i = kSizes - 1; i >= 0; --i) {
