@@ -368,7 +368,7 @@ struct PlainWarp {
   static_assert(kNext >= 1, "a lane has a piece of the queries");
   // The lanes that share rows split the queries when the logits are summed: each has kOwn of them, from own0() on.
   static constexpr int kOwn = Q / kSplit;
-  static_assert(kOwn >= 1 && kOwn * kSplit == Q, "queries of a lane");
+  static_assert((kOwn == 1 || kOwn == 2) && kOwn * kSplit == Q, "queries of a lane");
   uint4 next[kNext];      // of the queries of the next head
   float m[kOwn], l[kOwn], o[Q][kCols];
   static __device__ __forceinline__ int own0() { return (threadIdx.x & 31) / kLanes * kOwn; }
@@ -478,8 +478,7 @@ struct PlainWarp {
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       float* const to = probs + (row + j * kLanes) * Q + own0();
-      if constexpr (kOwn == 4) *reinterpret_cast<float4*>(to) = make_float4(z[j][0], z[j][1], z[j][2], z[j][3]);
-      else if constexpr (kOwn == 2) *reinterpret_cast<float2*>(to) = make_float2(z[j][0], z[j][1]);
+      if constexpr (kOwn == 2) *reinterpret_cast<float2*>(to) = make_float2(z[j][0], z[j][1]);
       else to[0] = z[j][0];
     }
     __syncwarp();
