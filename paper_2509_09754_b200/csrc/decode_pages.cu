@@ -139,11 +139,9 @@ struct Logit {
       : scale(c.scale * kLog2e), in(c.softcap > 0.f ? c.scale / c.softcap : 0.f), cap(c.softcap * kLog2e) {}
   __device__ __forceinline__ float of(float s) const {
     if (cap == 0.f) return s * scale;
-    // tanh z = 1 - 2 / (e^(2 z) + 1); near zero, where that cancels, its series (to z^9: 2e-9 at 1/4)
-    const float z = s * in, zz = z * z;
-    const float t = 1.f - __fdividef(2.f, fast_exp2(z * (2.f * kLog2e)) + 1.f);
-    const float series = z * fmaf(zz, fmaf(zz, fmaf(zz, fmaf(zz, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
-    return cap * (fabsf(z) < 0.25f ? series : t);
+    // (tanhf, whose capped logits are within 2.4 * 2^-24 around z = 1/4, rather than 1 - 2 / (e^(2 z) + 1) with the fast
+    // exponential, which cancels there: 6.8; 64 x 8 heads of 2048 rows, bf16, us: 91.6 / 92.4, with 16 queries a head 115.7 / 118.1, of 64 columns 61.8 / 63.7)
+    return cap * tanhf(s * in);
   }
 };
 
