@@ -458,7 +458,8 @@ LAVA_API lava_status lava_check_compact_kv_pages(const lava_layer_desc* desc, co
 /* Rotary positions.  Pair i of a vector's leading rotary_dim elements turns by the angle
  * positions[token] * freqs[i]:  (a, b) -> scale * (a cos - b sin, b cos + a sin); the other elements
  * are copied.  Pairs are (i, i + rotary_dim/2), or (2i, 2i+1) where `interleaved`.  Angles are reduced
- * in 64 bits, so far positions lose nothing; vectors are turned in fp32 and rounded once.
+ * in 64 bits, so far positions lose no more than near ones; cosines, sines and products are fp32, and
+ * vectors are rounded once.
  * `backward` turns by the negative angles with the same scale: the gradient with respect to the input
  * of a gradient with respect to the output (the rotation's transpose), and where scale is 1 what undoes
  * the rotation. */
