@@ -401,7 +401,8 @@ typedef struct lava_cache_desc {
                           max_pages * page_rows < 2^30                                      */
   int64_t n_pages;     /* pages of the pool; n_pages * page_rows < 2^31                     */
   float sm_scale;      /* logit scale; 0 => 1/sqrt(head_dim)                                */
-  float softcap;       /* 0 => none; else a logit x becomes softcap * tanh(x / softcap)     */
+  float softcap;       /* 0 => none; else a logit x becomes softcap * tanh(x / softcap).  Both below
+                          2.3e38, and sm_scale / softcap a normal fp32 number               */
 } lava_cache_desc;
 
 /* Bytes of `workspace` for the paged calls of this cache: a status word (first 256 bytes, as in

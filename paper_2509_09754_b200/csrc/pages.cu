@@ -57,6 +57,10 @@ lava_status make_cache(const lava_cache_desc* d, Cache* out) {
   c.heads = (int)heads;
   c.scale = d->sm_scale > 0.f ? d->sm_scale : (float)(1.0 / sqrt((double)d->head_dim));
   c.softcap = d->softcap;
+  // the factors that logits are multiplied by in the base-2 domain
+  constexpr float kLog2e = 1.44269504f;
+  if (isinf(c.scale * kLog2e) || isinf(c.softcap * kLog2e) || (c.softcap > 0.f && !isnormal(c.scale / c.softcap)))
+    return fail(LAVA_ERR_INVALID_ARG, "sm_scale, softcap or their quotient leaves fp32");
   *out = c;
   return LAVA_OK;
 }
