@@ -4,6 +4,7 @@
 // arguments' conversion; the rest is the launch.  The functions here take plain positional arguments from paged.py.
 #include <Python.h>
 
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -85,9 +86,31 @@ class Call {
     if (device_ < 0) device_ = c10::cuda::current_device();
     return t.get_device() == device_;
   }
+  // the next argument, which the call writes to
+  const at::Tensor* output(const char* name) {
+    const at::Tensor* t = tensor(name);
+    if (t && without_gradient(name, *t)) written_[n_written_++] = t;
+    return ok_ ? t : nullptr;
+  }
+  // The calls write through addresses, which autograd does not see: a tensor that it follows is refused.
+  bool without_gradient(const char* name, const at::Tensor& t) {
+    if (t.requires_grad() && c10::GradMode::is_enabled())
+      refuse(std::string(name) + " requires a gradient, which this call does not follow: torch.no_grad(), or its own backward");
+    return ok_;
+  }
+  // After the call: autograd asks whether what it saved was written to since.
+  void bump_versions() const {
+    for (int i = 0; i < n_written_; ++i)
+      if (!written_[i]->is_inference()) written_[i]->unsafeGetTensorImpl()->bump_version();
+  }
   // the address of a contiguous tensor of this type and shape on the current device
   void* buffer(const char* name, at::ScalarType type, std::initializer_list<int64_t> shape) {
-    const at::Tensor* t = tensor(name);
+    return buffer(name, tensor(name), type, shape);
+  }
+  void* written(const char* name, at::ScalarType type, std::initializer_list<int64_t> shape) {
+    return buffer(name, output(name), type, shape);
+  }
+  void* buffer(const char* name, const at::Tensor* t, at::ScalarType type, std::initializer_list<int64_t> shape) {
     if (!t) return nullptr;
     if (t->scalar_type() != type || t->sizes() != at::IntArrayRef(shape) || !here(*t) || !t->is_contiguous()) {
       refuse(std::string(name) + " must be a " + c10::toString(type) + " tensor of shape " + shape_text(shape) +
@@ -102,7 +125,9 @@ class Call {
     int64_t tok, head;
   };
   Vectors vectors(const char* name, at::ScalarType type, int64_t tokens, int64_t heads, int64_t dim) {
-    const at::Tensor* t = tensor(name);
+    return vectors(name, tensor(name), type, tokens, heads, dim);
+  }
+  Vectors vectors(const char* name, const at::Tensor* t, at::ScalarType type, int64_t tokens, int64_t heads, int64_t dim) {
     if (!t) return {};
     if (t->scalar_type() != type || t->sizes() != at::IntArrayRef({tokens, heads, dim}) || t->stride(2) != 1 || !here(*t)) {
       refuse(std::string(name) + " must be a " + c10::toString(type) + " tensor of shape " + shape_text({tokens, heads, dim}) +
@@ -143,16 +168,19 @@ class Call {
   Py_ssize_t at_ = 0;
   bool ok_ = true;
   int device_ = -1;
+  const at::Tensor* written_[4] = {};
+  int n_written_ = 0;
 };
 
 // Runs the C function without the interpreter's lock.
 template <class F>
-PyObject* finish(const F& f) {
+PyObject* finish(const Call& c, const F& f) {
   lava_status st;
   Py_BEGIN_ALLOW_THREADS
   st = f();
   Py_END_ALLOW_THREADS
   if (st != LAVA_OK) return raise_error(st, lava_last_error());
+  c.bump_versions();
   Py_RETURN_NONE;
 }
 
@@ -190,7 +218,7 @@ PyObject* page_admit(PyObject* const* args, Py_ssize_t n) {
   auto* counters_out = c.none() ? counters : (int64_t*)c.buffer("counters_out", at::kLong, {2});
   void* stream = c.stream();
   if (!c.ok()) return nullptr;
-  return finish([&] {
+  return finish(c, [&] {
     return lava_page_admit(d, first_seq, (int32_t)n_seqs, hoff, rows, rows_out, table, ring, counters, counters_out,
                            first_row, status, stream);
   });
@@ -218,7 +246,7 @@ PyObject* page_extend(PyObject* const* args, Py_ssize_t n) {
   auto* counters_out = c.none() ? counters : (int64_t*)c.buffer("counters_out", at::kLong, {2});
   void* stream = c.stream();
   if (!c.ok()) return nullptr;
-  return finish([&] {
+  return finish(c, [&] {
     return lava_page_extend(d, add, (int32_t)max_add, rows, rows_out, table, ring, counters, counters_out, slots, status,
                             stream);
   });
@@ -253,12 +281,12 @@ PyObject* compact_pages(PyObject* const* args, Py_ssize_t n) {
   const auto* hoff = (const int32_t*)c.buffer("head_offsets", at::kInt, {L, S, H + 1});
   const auto* first_row = (const int32_t*)c.buffer("first_row", at::kInt, {L, S, H});
   const auto* table = (const int32_t*)c.buffer("page_table", at::kInt, {L, d->batch, H, d->max_pages});
-  void* k_pages = c.buffer("k_pages", type, {d->n_pages, d->page_rows, D});
-  void* v_pages = c.buffer("v_pages", type, {d->n_pages, d->page_rows, D});
+  void* k_pages = c.written("k_pages", type, {d->n_pages, d->page_rows, D});
+  void* v_pages = c.written("v_pages", type, {d->n_pages, d->page_rows, D});
   void* stream = c.stream();
   if (!c.ok()) return nullptr;
   const void *k = kv[0]->data_ptr(), *v = kv[1]->data_ptr();
-  return finish([&] {
+  return finish(c, [&] {
     return CHECK ? lava_check_compact_kv_pages(layer, d, first_seq, k, v, k_ls, v_ls, keep, hoff, first_row, table, k_pages,
                                                v_pages)
                  : lava_compact_kv_pages(layer, d, first_seq, k, v, k_ls, v_ls, keep, hoff, first_row, table, k_pages,
@@ -301,13 +329,15 @@ PyObject* rotary(PyObject* const* args, Py_ssize_t n) {
       a.heads = t.dim() == 3 ? t.size(1) : 0;
     }
     if (a.heads > 0x7fffffff) c.refuse(std::string(a.in_name) + " has too many heads");
-    a.in = c.vectors(a.in_name, type, tokens, a.heads, r->head_dim);
+    const at::Tensor* in = c.tensor(a.in_name);
+    if (!in || !c.without_gradient(a.in_name, *in)) return nullptr;
+    a.in = c.vectors(a.in_name, in, type, tokens, a.heads, r->head_dim);
     if (c.ok() && c.peek() == Py_None) c.refuse(std::string(a.in_name) + " and " + a.out_name + " are both given or both None");
-    a.out = c.vectors(a.out_name, type, tokens, a.heads, r->head_dim);
+    a.out = c.vectors(a.out_name, c.output(a.out_name), type, tokens, a.heads, r->head_dim);
   }
   void* stream = c.stream();
   if (!c.ok()) return nullptr;
-  return finish([&] {
+  return finish(c, [&] {
     return lava_rotary(r, freqs, tokens, positions, x[0].in.at, (int32_t)x[0].heads, x[0].in.tok, x[0].in.head, x[0].out.at,
                        x[0].out.tok, x[0].out.head, x[1].in.at, (int32_t)x[1].heads, x[1].in.tok, x[1].in.head, x[1].out.at,
                        x[1].out.tok, x[1].out.head, stream);
@@ -338,12 +368,12 @@ PyObject* rotary_append(PyObject* const* args, Py_ssize_t n) {
   const auto* positions = (const int32_t*)c.buffer("positions", at::kInt, {tokens});
   const auto q = c.vectors("q", type, tokens, Hq, D), k = c.vectors("k", type, tokens, H, D),
              v = c.vectors("v", type, tokens, H, D);
-  void* q_out = c.buffer("q_out", type, {tokens, Hq, D});
-  void* k_pages = c.buffer("k_pages", type, {d->n_pages, d->page_rows, D});
-  void* v_pages = c.buffer("v_pages", type, {d->n_pages, d->page_rows, D});
+  void* q_out = c.written("q_out", type, {tokens, Hq, D});
+  void* k_pages = c.written("k_pages", type, {d->n_pages, d->page_rows, D});
+  void* v_pages = c.written("v_pages", type, {d->n_pages, d->page_rows, D});
   void* stream = c.stream();
   if (!c.ok()) return nullptr;
-  return finish([&] {
+  return finish(c, [&] {
     return lava_rotary_append(r, freqs, d, tokens, positions, q.at, q.tok, q.head, q_out, k.at, k.tok, k.head, v.at, v.tok,
                               v.head, slots + layer * tokens * H, k_pages, v_pages, stream);
   });
@@ -367,15 +397,15 @@ PyObject* decode_attention_pages(PyObject* const* args, Py_ssize_t n) {
   const void* v_pages = c.buffer("v_pages", type, {d->n_pages, d->page_rows, D});
   const auto* table = (const int32_t*)c.buffer("page_table", at::kInt, {L, B, H, d->max_pages});
   const auto* rows = (const int32_t*)c.buffer("head_rows", at::kInt, {L, B, H});
-  void* out = c.buffer("out", type, {layers, B, Hq, D});
-  auto* lse = c.none() ? nullptr : (float*)c.buffer("lse", at::kFloat, {layers, B, Hq});
+  void* out = c.written("out", type, {layers, B, Hq, D});
+  auto* lse = c.none() ? nullptr : (float*)c.written("lse", at::kFloat, {layers, B, Hq});
   const at::Tensor* ws = c.tensor("workspace");
   if (ws && (!c.here(*ws) || !ws->is_contiguous())) c.refuse("workspace must be contiguous and on the current device");
   void* stream = c.stream();
   if (!c.ok()) return nullptr;
   void* ws_at = ws->data_ptr();
   const size_t ws_bytes = ws->nbytes();
-  return finish([&] {
+  return finish(c, [&] {
     return lava_decode_attention_pages(d, first_layer, (int32_t)layers, q, k_pages, v_pages, table, rows, out, lse, ws_at,
                                        ws_bytes, stream);
   });

@@ -2,7 +2,7 @@
 
 The functions carry the names of the C ABI in include/lava.h, which describes the arguments.  They go through a small
 native module (csrc/paged_calls.cpp) that looks into the tensors and refuses a wrong type, shape, layout or device with
-a LavaError before the C function sees them.
+a LavaError before the C function sees them.  What they write carries no gradient.
 """
 from __future__ import annotations
 
@@ -162,7 +162,9 @@ def lava_rotary_freqs(rotary_dim: int, base: float = 10000.0, kind: int = LAVA_R
 
 
 def lava_rotary(rotary: RotaryDesc, freqs, positions, q, k, q_out, k_out, stream=None) -> None:
-    """Queries and keys [n_tokens, heads, head_dim] (any strides of tokens and heads) turned into q_out and k_out."""
+    """Queries and keys [n_tokens, heads, head_dim] (any strides of tokens and heads) turned into q_out and k_out.
+    Autograd does not follow the call, so tensors that require a gradient are refused where it records: a
+    torch.autograd.Function turns in its forward, and the gradients with RotaryDesc(backward=True) in its backward."""
     (_CALLS or load_paged_calls()).rotary(rotary._at, freqs, positions, q, q_out, k, k_out, _handle(stream))
 
 
