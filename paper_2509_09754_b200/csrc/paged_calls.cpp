@@ -174,13 +174,13 @@ class Call {
 
 // Runs the C function without the interpreter's lock.
 template <class F>
-PyObject* finish(const Call& c, const F& f) {
+PyObject* finish(const Call& c, const F& f, bool writes = true) {
   lava_status st;
   Py_BEGIN_ALLOW_THREADS
   st = f();
   Py_END_ALLOW_THREADS
   if (st != LAVA_OK) return raise_error(st, lava_last_error());
-  c.bump_versions();
+  if (writes) c.bump_versions();
   Py_RETURN_NONE;
 }
 
@@ -291,7 +291,7 @@ PyObject* compact_pages(PyObject* const* args, Py_ssize_t n) {
                                                v_pages)
                  : lava_compact_kv_pages(layer, d, first_seq, k, v, k_ls, v_ls, keep, hoff, first_row, table, k_pages,
                                          v_pages, stream);
-  });
+  }, !CHECK);
 }
 PyObject* compact_kv_pages(PyObject* const* args, Py_ssize_t n) { return compact_pages<false>(args, n); }
 PyObject* check_compact_kv_pages(PyObject* const* args, Py_ssize_t n) { return compact_pages<true>(args, n); }

@@ -94,3 +94,17 @@ def test_a_step_of_the_cache_marks_what_it_writes():
         cache.attend(0, q, out.requires_grad_(), lse)
     with torch.no_grad():
         cache.attend(0, q, out, lse)
+
+
+@pytest.mark.gpu
+def test_an_admission_marks_the_pages_once():
+    k = torch.randn((1, 2, 200, 64), device="cuda")
+    q = torch.randn((1, 1, 8, 16, 64), device="cuda")
+    plan = lava.EvictionPlan.create(lava.LayerDesc.for_tensors(q[0], k[0], k[0], 16, max_seqlen=200), 1, [128], [200],
+                                    kv_dtype=torch.float32)
+    cache = lava.PagedCache(lava.CacheDesc(n_layers=1, batch=1, n_q_heads=8, n_kv_heads=2, head_dim=64, max_pages=16, n_pages=16,
+                                           page_rows=16, dtype=lava.LAVA_F32))
+    before = cache.k_pages._version, cache.v_pages._version
+    cache.evict(plan, q, k, k)
+    assert (cache.k_pages._version, cache.v_pages._version) == (before[0] + 1, before[1] + 1)
+    assert cache.poll_status() == 0 and int(cache.head_rows.sum()) == 128
