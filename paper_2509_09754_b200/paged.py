@@ -216,7 +216,9 @@ class PagedCache:
         self._slots = {}
 
     def free_page_count(self) -> int:
-        """Pages that are free; waits for the device."""
+        """Pages that are free; waits for the device, whatever streams the calls before were on."""
+        if self.counters.is_cuda:
+            torch.cuda.synchronize(self.counters.device)
         taken, given = self.counters.tolist()
         return given - taken
 
