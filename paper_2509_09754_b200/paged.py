@@ -208,8 +208,9 @@ class PagedCache:
         self.head_rows = torch.zeros(heads, **i32)
         self.page_table = torch.full(heads + (desc.max_pages,), -1, **i32)
         self.free_pages = torch.arange(desc.n_pages, **i32)
-        self.counters = torch.tensor([0, desc.n_pages], dtype=torch.int64, device=device)
         self.workspace = torch.zeros(need, dtype=torch.uint8, device=device)
+        # (last: this copy from the host waits for what the stream had before it, so any stream may use the cache now)
+        self.counters = torch.tensor([0, desc.n_pages], dtype=torch.int64, device=device)
         self.slots = None  # of the last extend
         # by number of rows: a captured extend keeps their address, and a stream may be behind the one that calls next, so
         # none is given up while the cache lives

@@ -34,6 +34,17 @@ def test_append_reads_the_slots_of_the_last_extend(cache):
         assert cache.slots is slots and slots.shape == (2, 3, n, 2) and bool((slots == n).all())
 
 
+def test_the_copy_that_waits_is_the_last_of_a_new_cache(monkeypatch):
+    """Every other buffer is filled on the current stream without waiting for it."""
+    calls = []
+    for name in ("empty", "zeros", "full", "arange", "tensor"):
+        f = getattr(torch, name)
+        monkeypatch.setattr(torch, name, lambda *a, _f=f, _n=name, **kw: (calls.append(_n), _f(*a, **kw))[1])
+    lava.PagedCache(lava.CacheDesc(n_layers=1, batch=1, n_q_heads=2, n_kv_heads=1, head_dim=64, max_pages=1, n_pages=1),
+                    device="cpu")
+    assert "tensor" not in calls[:-1] and calls[-1] == "tensor"
+
+
 @pytest.mark.gpu
 def test_a_captured_step_keeps_its_slots():
     """A step of one token in a graph; five rows eagerly; memory of the slots' size filled; the step replayed."""
