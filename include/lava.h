@@ -520,7 +520,8 @@ LAVA_API lava_status lava_rotary_append(const lava_rotary_desc* rotary, const do
  * g = h / (H_q / H_kv) of its sequence:
  *     x_i = sm_scale * q[h] . K_g[i]   (capped where softcap > 0),   i < head_rows
  *     out[h] = softmax_i(x_i) V_g,     lse[h] = ln sum_i exp(x_i)
- * for layers first_layer ... first_layer + n_layers - 1 in one call.
+ * for layers first_layer ... first_layer + n_layers - 1 in one call.  Of the tokens that one
+ * lava_page_extend made room for (max_add > 1) only the last may see all the rows: it is the one to attend.
  *   q, out      [n_layers, batch, H_q, d], dtype cache->dtype; they must not overlap
  *   lse         float [n_layers, batch, H_q], may be NULL
  *   page_table, head_rows   of the whole cache; they must not change while the call runs
@@ -528,7 +529,7 @@ LAVA_API lava_status lava_rotary_append(const lava_rotary_desc* rotary, const do
  * The heads of a call times max_pages * page_rows stay below 2^35 (times the portions of 16 queries, 8 with
  * fp32, that a group has).  A head without rows gives zeros and lse = -infinity.  Sums, maxima and the output before its last
  * rounding are fp32; with bf16 the probabilities enter the product with V as two bf16 terms (relative
- * error below 2^-16).  The split of the rows over blocks depends on all row counts of the call, so the
+ * error below 2^-16), so an infinity in V may come out as NaN.  The split of the rows over blocks depends on all row counts of the call, so the
  * last bits may too; the same call gives the same bits. */
 LAVA_API lava_status lava_decode_attention_pages(const lava_cache_desc* cache, int32_t first_layer,
                                                  int32_t n_layers, const void* q, const void* k_pages,

@@ -2,8 +2,9 @@
 //
 // The rows of all (layer, sequence, KV head) in their order are one line, which is cut into equal runs of consecutive
 // rows, a run per warp: heads keep uneven numbers of rows (up to eight times the mean), and with blocks per head, as
-// the packed compaction has them, the longest is waited for.  Blocks per head / runs, us: 32 layers x 32K, 524288 rows
-// 110 / 95; 8K, 131072 rows 35.5 / 21.7; 1K, 32768 rows 9.6 / 7.4; ragged batch of 8, 262144 rows 52.8 / 52.7.  Row
+// the packed compaction has them, the longest is waited for.  Blocks per head / runs, us on the device, one prompt again
+// and again: 32 layers x 32K, 524288 rows 110 / 95; 8K, 131072 rows 35.5 / 21.7; 1K, 32768 rows 9.6 / 7.4; ragged batch of
+// 8, 262144 rows 52.8 / 52.7.  (Runs, several prompts in turn, so that nothing of one is in L2: 96, 28.5, 8.1.)  Row
 // counts live on the device, so every warp finds its run itself, from the rows of the problems (layer, sequence).
 //
 // A lane looks up a row: its head, its position (kept list or window), its page; for the next 32 rows while these are

@@ -15,15 +15,15 @@
 // through the memory of the last stage.  A head inside one part is finished there.  Of a head that continues in other
 // parts the partial result goes to memory; the CTA that comes last, as a counter tells, joins them in order.
 //
-// bf16: S = Q K^T and O += P V by mma.sync m16n8k16 (2 % of the tensor peak at the rate of HBM).  With up to 8 queries
-// the other 8 rows of the A operand are free: they carry what rounding the probabilities to bf16 left over, so the
-// products with V keep 16 bits of every probability at no cost; with 9 to 16 queries a second product does.  More
+// bf16: S = Q K^T and O += P V by mma.sync m16n8k16 (the tensor pipe is 18 % busy at the rate of HBM).  With up to 8
+// queries the other 8 rows of the A operand are free: they carry what rounding the probabilities to bf16 left over, so
+// the products with V keep 16 bits of every probability at no cost; with 9 to 16 queries a second product does.  More
 // queries per KV head than 16 are taken 16 at a time.  fp32: lanes have a share of one or two rows for the logits, and
 // some columns for the product with V; up to 8 queries at a time.
 //
-// Bound by HBM where the heads hold enough (64 x 8 heads of 2048 rows, bf16 of 128: 91 us, 5.8 TB/s where a copy has
-// 6.6; 16 queries a head 105 us; fp32, 32 sequences: 87 us, with 8 queries a head 93), else by the chain of one CTA:
-// counts, page table, rows, joining (5.6 us for short sequences, 8 where heads are split).
+// Bound by HBM where the heads hold enough (64 x 8 heads of 2048 rows, bf16 of 128: 92 us, 5.8 TB/s where a copy has
+// 6.6; 16 queries a head 106 us; fp32, 32 sequences: 88 us, with 8 queries a head 93), else by the chain of one CTA:
+// counts, page table, rows, joining (5.5 us for short sequences, 8 to 10 where heads are split).
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -139,8 +139,9 @@ struct Logit {
       : scale(c.scale * kLog2e), in(c.softcap > 0.f ? c.scale / c.softcap : 0.f), cap(c.softcap * kLog2e) {}
   __device__ __forceinline__ float of(float s) const {
     if (cap == 0.f) return s * scale;
-    // (tanhf, whose capped logits are within 2.4 * 2^-24 around z = 1/4, rather than 1 - 2 / (e^(2 z) + 1) with the fast
-    // exponential, which cancels there: 6.8; 64 x 8 heads of 2048 rows, bf16, us: 91.6 / 92.4, with 16 queries a head 115.7 / 118.1, of 64 columns 61.8 / 63.7)
+    // (tanhf: around z = 1/4 capped logits are off by 2.4 * 2^-24 of themselves.  1 - 2 / (e^(2 z) + 1) with the fast
+    // exponential cancels there, 6.8.  That / tanhf, us, 64 x 8 heads of 2048 rows, bf16: 91.6 / 92.4; with 16 queries a
+    // head 115.7 / 118.1; of 64 columns 61.8 / 63.7.)
     return cap * tanhf(s * in);
   }
 };

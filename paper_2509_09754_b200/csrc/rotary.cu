@@ -10,7 +10,8 @@
 // to fp32 there, up to 9.4e-8 rad, is put back to first order where vectors are fp32: a cosine or sine is off by its own
 // rounding then, 1.5 * 2^-24.  Not with bf16, whose outputs are rounded by 2^-9 to 2^-8 (1024 tokens 5.2 us, with it 5.6).
 //
-// Bound by reading and writing the vectors once: 6.2 TB/s at 32K tokens, where a copy has 6.6 (1K tokens stay in L2: 5.2 us).
+// Bound by reading and writing the vectors once: 108 to 110 us at 32K tokens, 6.1 to 6.2 TB/s where a copy has 6.6 (1K
+// tokens stay in L2: 5.2 us).
 #include <algorithm>
 
 #include <math.h>

@@ -187,6 +187,7 @@ def lava_decode_attention_pages(cache: CacheDesc, first_layer, q, k_pages, v_pag
 class PagedCache:
     """A paged cache and its buffers.  A prompt enters with `admit` after its selection (or with `evict`, which
     scores and selects as well); then, for every token, `extend` once and `append` and `attend` layer by layer.
+    Its calls share tables and a workspace: they follow one another, on one stream or on streams that wait.
 
         cache = PagedCache(lava.CacheDesc(n_layers=32, batch=8, n_q_heads=32, n_kv_heads=8, head_dim=128,
                                           max_pages=512, n_pages=65536))
@@ -269,7 +270,8 @@ class PagedCache:
         return q_out
 
     def attend(self, first_layer: int, q, out=None, lse=None, stream=None):
-        """(out, lse) of q [batch, H_q, d] or [n_layers, batch, H_q, d] over the rows that the heads hold."""
+        """(out, lse) of q [batch, H_q, d] or [n_layers, batch, H_q, d] over all the rows that the heads hold: one query
+        per sequence, its last token's where `extend` made room for several."""
         one = q.dim() == 3
         q = q.unsqueeze(0) if one else q
         out = _empty(q.shape, q.dtype, q.device, stream) if out is None else out.view(q.shape)
